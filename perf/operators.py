@@ -20,7 +20,7 @@ own = False   # True: the framework's entry points; False: plain torch operation
 
 DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
 LARGEST = {0: 127, 8: 127, 4: 7}
-SMALLEST_ROW = 2.0 ** -120   # rows whose largest magnitude is below this are stored as zeros
+SMALLEST_ROW = 2.0 ** -100   # rows whose largest magnitude is below this are stored as zeros
 
 
 def cache(name, **more):
