@@ -478,6 +478,99 @@ sti_status sti_quantize_layer(const sti_dims *dims, const float *weights, int bi
                               sti_quant_stats *stats, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * Keys and values of earlier tokens, kept in pages, and the attention of new tokens over
+ * them: for a program that feeds a submodel token by token or chunk by chunk instead of whole
+ * sequences.  Causal; any number of sequences, each with any number of new tokens per call,
+ * none included.
+ *
+ * Pages.  A pool holds n_pages pages of page_tokens token slots, for keys and for values:
+ *     row(page, head, slot) = ((page * n_kv_heads + head) * page_tokens + slot)
+ * is d_head values of one token and one key/value head: `bits` 16: of type `dtype`; 8: signed
+ * bytes; 4: two codes plus 8 to a byte, the first value's in the low half.  For 8 and 4 bits
+ * k_scale[row] and v_scale[row] (float32) are what a code of 1 stands for.  Position p of
+ * sequence b lies in slot p % page_tokens of page page_table[b][p / page_tokens].  Entries of
+ * the table outside [0, n_pages) name no page: nothing is written or read through them, and the
+ * positions behind them are not seen by any query (so a window's user may drop old pages).
+ *
+ * Batch.  lengths[b] counts the tokens of sequence b with the new ones; the new tokens of all
+ * sequences lie row by row, those of b in rows offsets[b] .. offsets[b+1] (offsets[0] = 0,
+ * not decreasing, offsets[n_seqs] = n_tokens; lengths and offsets are read on the device, where
+ * rows outside [0, n_tokens) and positions outside [0, max_pages * page_tokens) are
+ * left out).  They are the last of the sequence: row r has position
+ * lengths[b] - (offsets[b+1] - r); one below 0 is not stored, and sees nothing.
+ *
+ * n_kv_heads 1 .. 64; d_head 64 or 128; page_tokens a power of two, 16 .. 1024 (STI_ERR_DIMS).
+ * k, v 16-byte, scales, page_table, lengths, offsets 4-byte aligned.  Calls take part in the
+ * order of their streams only: an append and the attention that reads it go to one stream, or
+ * are ordered by the caller's events.  All calls enqueue kernels only and may be captured into a
+ * graph; lengths, offsets and table may change between replays, sizes may not.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int32_t n_kv_heads, d_head, bits, page_tokens, n_pages;
+    sti_dtype dtype;         /* bits 16: STI_F16 or STI_BF16 (STI_ERR_DTYPE); ignored otherwise      */
+    void *k, *v;             /* DEVICE [n_pages][n_kv_heads][page_tokens][d_head * bits / 8 bytes]   */
+    float *k_scale, *v_scale; /* DEVICE [n_pages][n_kv_heads][page_tokens]; ignored for 16 bits      */
+} sti_cache;
+
+typedef struct {
+    int32_t n_seqs, n_tokens, max_pages;
+    const int32_t *page_table; /* DEVICE [n_seqs][max_pages]                                          */
+    const int32_t *lengths;    /* DEVICE [n_seqs]                                                     */
+    const int32_t *offsets;    /* DEVICE [n_seqs + 1]; sti_cache_read does not use it                 */
+} sti_cache_batch;
+
+/* New tokens' keys and values into their slots.  With a = max |x| of a row, t = 127 (8 bits) or 7
+ * (4 bits), everything in float32:
+ *     scale = a * (1 / t),   code = x * (1 / scale) rounded to nearest even
+ * a below 2^-100: scale and codes 0; a NaN or infinity in the row: scale NaN, codes 0, so that the
+ * row reads back as NaN.  16 bits: each value rounded to `dtype` to nearest even.
+ *
+ *  k, v      DEVICE, rows [n_tokens] of n_kv_heads * d_head values of io_dtype (any sti_dtype), row r
+ *            at k + r * k_stride (strides in values, >= n_kv_heads * d_head: slices of one projection's
+ *            output do); base addresses and row strides multiples of 16 bytes (STI_ERR_ALIGN).
+ * Slots of two rows of a call must differ.
+ *
+ * Errors: NULL / DIMS / BITWIDTH (bits) / ALIGN / DTYPE / HIP. */
+sti_status sti_cache_append(const sti_cache *cache, const sti_cache_batch *batch, const void *k, const void *v,
+                            sti_dtype io_dtype, int64_t k_stride, int64_t v_stride, void *hip_stream);
+
+/* Positions first .. first + count - 1 of every sequence back as values:
+ *     k_out[b][j][head][:] = code * scale rounded once to out_dtype (16 bits: converted)
+ * and zeros at positions from lengths[b] on and where the table names no page.
+ *  k_out, v_out  DEVICE [n_seqs][count][n_kv_heads][d_head] of out_dtype, 16-byte aligned.
+ * Errors: NULL / DIMS / BITWIDTH / ALIGN / DTYPE / HIP. */
+sti_status sti_cache_read(const sti_cache *cache, const sti_cache_batch *batch, int32_t first, int32_t count, void *k_out,
+                          void *v_out, sti_dtype out_dtype, void *hip_stream);
+
+/* Attention of the new tokens over their sequences.  The query at position p of a sequence sees key
+ * j < lengths[b] when j <= p and, with window > 0, j > p - window or j < sinks; query head h reads
+ * key/value head h / (n_heads / n_kv_heads):
+ *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale * q . k_j - max)
+ * and zeros for a query that sees no key.  Keys and values that a query does not see have no part in
+ * its result, whatever they hold.  Products of queries with stored values or codes and their sums are float32,
+ * as are maxima, sums and the result until its one rounding; with many queries per sequence the weights w_j are
+ * rounded to io_dtype (the operand type of the matrix cores) before they multiply the values, their sum is not.
+ *
+ *  n_heads      a multiple of n_kv_heads, <= 512
+ *  q, out       DEVICE, rows [n_tokens] of n_heads * d_head values of io_dtype (STI_F16 or STI_BF16;
+ *               that of the cache when it holds 16 bits, STI_ERR_UNSUPPORTED otherwise), strides and
+ *               alignment as for sti_cache_append; not aliased.  Rows of no sequence stay as they are.
+ *  scale        > 0 and finite, or 0 for 1 / sqrt(d_head) (STI_ERR_DIMS)
+ *  window       >= 0, 0: all earlier tokens;  sinks >= 0, without meaning when window is 0
+ *  workspace    DEVICE, >= sti_cache_attention_workspace_bytes of the same sizes, 16-byte aligned; may
+ *               be NULL when that is 0.  It is that of partial results where few queries read long
+ *               sequences; what it is follows from the sizes in the structs, not from lengths.
+ * The query function reads no DEVICE memory and returns 0 for invalid arguments.
+ *
+ * Errors: NULL / DIMS / BITWIDTH / ALIGN / DTYPE / UNSUPPORTED / WORKSPACE / HIP. */
+size_t sti_cache_attention_workspace_bytes(const sti_cache *cache, const sti_cache_batch *batch, int32_t n_heads, int32_t window,
+                                           int32_t sinks);
+
+sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *batch, const void *q, void *out, sti_dtype io_dtype,
+                               int64_t q_stride, int64_t out_stride, int32_t n_heads, float scale, int32_t window, int32_t sinks,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing (the counterpart of the paper's one-time hardware profiling
  * of computation delays, Section "Prerequisite: offline profiling").  Between
  * sti_profile_begin() and sti_profile_end() every kernel launch of the entry
@@ -490,7 +583,7 @@ sti_status sti_quantize_layer(const sti_dims *dims, const float *weights, int bi
  * decompression of float32 weights beside it (d_model up to 1024), as a launch of
  * either class with half the time, so that the classes add up to one launch more
  * than was made, and to the time that was taken; the halves say nothing about the
- * two parts.
+ * two parts.  The calls on a cache count as attention, and as convert (append, read).
  * Process wide, not re-entrant; meant for measurement runs, not for production
  * calls (nor for calls under stream capture).
  * ------------------------------------------------------------------------- */

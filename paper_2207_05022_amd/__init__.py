@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     sti_decode_workspace_bytes, sti_decode_shards, sti_workspace_bytes,
     sti_layer_forward, sti_model_forward, sti_layer_forward_masked, sti_model_forward_masked, sti_profile_begin, sti_profile_end, sti_pipeline_staging_bytes, sti_model_workspace_bytes, sti_plan_submodel, sti_plan_bitwidths, sti_quantize_workspace_bytes, sti_quantize_layer, StiQuantStats, StiPipeline, StiPipelineStats, make_store, shard_array, sti_layer_forward_static,
     sti_working_buffer_bytes, sti_working_buffer_offset, sti_decode_working_buffer,
+    StiCache, StiCacheBatch, StiCacheStruct, StiCacheBatchStruct, sti_cache_append, sti_cache_read,
+    sti_cache_attention_workspace_bytes, sti_cache_attention,
 )

@@ -60,6 +60,17 @@ class StiQuantStats(C.Structure):
     _fields_ = [("mean", C.c_double), ("variance", C.c_double), ("n_outliers", C.c_uint64), ("status", C.c_uint32)]
 
 
+class StiCacheStruct(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("bits", C.c_int32), ("page_tokens", C.c_int32),
+                ("n_pages", C.c_int32), ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class StiCacheBatchStruct(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_pages", C.c_int32), ("page_table", C.c_void_p),
+                ("lengths", C.c_void_p), ("offsets", C.c_void_p)]
+
+
 class StiError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -142,6 +153,19 @@ def _load():
         C.c_void_p, C.POINTER(StiPipelineStats)]
     L.sti_pipeline_destroy.restype = C.c_int
     L.sti_pipeline_destroy.argtypes = [C.c_void_p]
+    L.sti_cache_append.restype = C.c_int
+    L.sti_cache_append.argtypes = [C.POINTER(StiCacheStruct), C.POINTER(StiCacheBatchStruct), C.c_void_p, C.c_void_p, C.c_int,
+                                   C.c_int64, C.c_int64, C.c_void_p]
+    L.sti_cache_read.restype = C.c_int
+    L.sti_cache_read.argtypes = [C.POINTER(StiCacheStruct), C.POINTER(StiCacheBatchStruct), C.c_int32, C.c_int32, C.c_void_p,
+                                 C.c_void_p, C.c_int, C.c_void_p]
+    L.sti_cache_attention_workspace_bytes.restype = C.c_size_t
+    L.sti_cache_attention_workspace_bytes.argtypes = [C.POINTER(StiCacheStruct), C.POINTER(StiCacheBatchStruct), C.c_int32,
+                                                      C.c_int32, C.c_int32]
+    L.sti_cache_attention.restype = C.c_int
+    L.sti_cache_attention.argtypes = [C.POINTER(StiCacheStruct), C.POINTER(StiCacheBatchStruct), C.c_void_p, C.c_void_p, C.c_int,
+                                      C.c_int64, C.c_int64, C.c_int32, C.c_float, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]
     L.sti_profile_begin.restype = C.c_int
     L.sti_profile_begin.argtypes = []
     L.sti_profile_end.restype = C.c_int
@@ -535,3 +559,100 @@ def sti_quantize_layer(dims, weights, bitwidth: int, packed, codebook, outlier_p
                                 _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_quantize_layer")
+
+
+class StiCache:
+    """Pool of pages of cached keys and values (sti_cache).  k, v: CUDA tensors [n_pages, n_kv_heads, page_tokens, row], contiguous:
+    float16 or bfloat16 with row = d_head (16 bits), int8 with row = d_head (8 bits) or uint8 with row = d_head / 2 (4 bits; the
+    last two with k_scale, v_scale: float32 [n_pages, n_kv_heads, page_tokens]).  The tensors are kept alive and written in place."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        bits = {torch.float16: 16, torch.bfloat16: 16, torch.int8: 8, torch.uint8: 4}.get(k.dtype)
+        if bits is None or k.dtype != v.dtype:
+            raise ValueError("a cache holds float16, bfloat16, int8 or uint8 (4 bits), keys and values alike")
+        if k.dim() != 4 or k.shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be contiguous [n_pages, n_kv_heads, page_tokens, row] of one shape")
+        if bits < 16:
+            for s in (k_scale, v_scale):
+                if s is None or s.dtype != torch.float32 or s.shape != k.shape[:3] or not s.is_contiguous():
+                    raise ValueError("codes need k_scale and v_scale, contiguous float32 [n_pages, n_kv_heads, page_tokens]")
+        else:
+            k_scale = v_scale = None
+        self.k, self.v, self.k_scale, self.v_scale, self.bits = k, v, k_scale, v_scale, bits
+        self.n_pages, self.n_kv_heads, self.page_tokens = (int(n) for n in k.shape[:3])
+        self.d_head = int(k.shape[3]) * (2 if bits == 4 else 1)
+        self.struct = StiCacheStruct(self.n_kv_heads, self.d_head, bits, self.page_tokens, self.n_pages,
+                                     _dtype_code(k) if bits == 16 else 0, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self.ref = C.byref(self.struct)
+
+
+class StiCacheBatch:
+    """Which rows of a call are whose (sti_cache_batch): CUDA int32 tensors page_table [n_seqs, max_pages], lengths [n_seqs],
+    offsets [n_seqs + 1] (None for sti_cache_read alone), contiguous and kept alive; their contents may change between calls."""
+
+    def __init__(self, page_table, lengths, offsets, n_tokens: int):
+        import torch
+        n_seqs = int(lengths.shape[0])
+        shapes = ((page_table, 2), (lengths, 1)) + (((offsets, 1),) if offsets is not None else ())
+        for t, dims in shapes:
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
+                raise ValueError("page_table, lengths and offsets must be contiguous int32 tensors of 2, 1 and 1 dimensions")
+        if page_table.shape[0] != n_seqs or (offsets is not None and offsets.shape[0] != n_seqs + 1):
+            raise ValueError("page_table has a row, and offsets an entry and one more, for each of lengths")
+        self.page_table, self.lengths, self.offsets = page_table, lengths, offsets
+        self.n_seqs, self.n_tokens, self.max_pages = n_seqs, int(n_tokens), int(page_table.shape[1])
+        self.struct = StiCacheBatchStruct(n_seqs, self.n_tokens, self.max_pages, _ptr(page_table), _ptr(lengths), _ptr(offsets))
+        self.ref = C.byref(self.struct)
+
+
+def _row_stride(t, batch, heads: int, d_head: int, name: str) -> int:
+    """Stride between the rows of t [n_tokens, heads, d_head], whose rows lie as one piece each."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[1] != heads or shape[2] != d_head:
+        raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {d_head}], not {list(shape)}")
+    if (strides[2] != 1 and d_head > 1) or (strides[1] != d_head and heads > 1):
+        raise ValueError(f"the values of a row of {name} must lie behind each other")
+    return strides[0] if shape[0] > 1 else heads * d_head
+
+
+def sti_cache_append(cache: StiCache, batch: StiCacheBatch, k, v, stream=None) -> None:
+    """k, v: CUDA tensors [n_tokens, n_kv_heads, d_head] of one dtype (float32, float16, bfloat16); rows may lie apart."""
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must have one dtype")
+    heads, d = cache.n_kv_heads, cache.d_head
+    st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k),
+                              _row_stride(k, batch, heads, d, "k"), _row_stride(v, batch, heads, d, "v"), _stream_handle(stream))
+    if st != 0:
+        raise StiError(st, "sti_cache_append")
+
+
+def sti_cache_read(cache: StiCache, batch: StiCacheBatch, first: int, k_out, v_out, stream=None) -> None:
+    """k_out, v_out: contiguous CUDA tensors [n_seqs, count, n_kv_heads, d_head] of one dtype, for positions first .. first + count - 1."""
+    shape = k_out.shape
+    if len(shape) != 4 or shape != v_out.shape or shape[0] != batch.n_seqs or shape[2] != cache.n_kv_heads or shape[3] != cache.d_head:
+        raise ValueError("k_out and v_out must be [n_seqs, count, n_kv_heads, d_head]")
+    if k_out.dtype != v_out.dtype or not k_out.is_contiguous() or not v_out.is_contiguous():
+        raise ValueError("k_out and v_out must be contiguous and of one dtype")
+    st = lib.sti_cache_read(cache.ref, batch.ref, int(first), shape[1], k_out.data_ptr(), v_out.data_ptr(), _dtype_code(k_out),
+                            _stream_handle(stream))
+    if st != 0:
+        raise StiError(st, "sti_cache_read")
+
+
+def sti_cache_attention_workspace_bytes(cache: StiCache, batch: StiCacheBatch, n_heads: int, window: int = 0, sinks: int = 0) -> int:
+    return int(lib.sti_cache_attention_workspace_bytes(cache.ref, batch.ref, int(n_heads), int(window), int(sinks)))
+
+
+def sti_cache_attention(cache: StiCache, batch: StiCacheBatch, q, out, workspace=None, scale: float = 0.0, window: int = 0,
+                        sinks: int = 0, stream=None) -> None:
+    """q, out: CUDA tensors [n_tokens, n_heads, d_head] of float16 or bfloat16 (the cache's type when it holds 16 bits); rows may lie
+    apart.  workspace: CUDA uint8 tensor of sti_cache_attention_workspace_bytes, or None where that is 0."""
+    if q.dtype != out.dtype:
+        raise ValueError("q and out must have one dtype")
+    heads, d = q.shape[1], cache.d_head
+    st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), _row_stride(q, batch, heads, d, "q"),
+                                 _row_stride(out, batch, heads, d, "out"), heads, scale, window, sinks, _ptr(workspace),
+                                 _nbytes(workspace), _stream_handle(stream))
+    if st != 0:
+        raise StiError(st, "sti_cache_attention")

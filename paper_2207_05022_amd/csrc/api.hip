@@ -161,6 +161,19 @@ hipError_t timed(int cls, hipStream_t stream, F fn, int also = -1)
     return e;
 }
 
+sti_status begin_timed(int cls)
+{
+    Profiler &pr = profiler();
+    if (pr.enabled()) STI_TRY(pr.next(cls, -1, &pending_launch_events));
+    return STI_OK;
+}
+void end_timed()
+{
+    Profiler &pr = profiler();
+    if (pr.enabled() && pending_launch_events.start == nullptr) pr.commit();
+    pending_launch_events = LaunchEvents{};
+}
+
 LaunchEvents take_launch_events()
 {
     const LaunchEvents ev = pending_launch_events;

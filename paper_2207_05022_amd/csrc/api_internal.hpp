@@ -13,6 +13,10 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
         if ((expr) != hipSuccess) return STI_ERR_HIP; \
     } while (0)
 
+// Around one launch of an entry point outside api.hip: its events, of kernel class `cls`, while per-kernel timing is on.
+sti_status begin_timed(int cls);
+void end_timed();
+
 constexpr size_t kStaticScratchBytes = (size_t)64 << 20;   // of sti_layer_forward_static
 
 // Offsets of the scratch regions of one layer call inside the caller's workspace.

@@ -1,0 +1,174 @@
+// Entry points of the paged key/value cache: argument checks, device views, which kernel a call takes.
+#include <math.h>
+#include "api_internal.hpp"
+#include "cache_common.hpp"
+
+using namespace sti;
+
+namespace {
+
+constexpr int64_t kMostPositions = (int64_t)1 << 30;   // of a sequence: sums and differences of positions and windows fit 32 bits
+constexpr int64_t kMostTokens = (int64_t)1 << 24;      // new tokens of a call
+constexpr int64_t kMostBlocks = 0x7FFFFFFF;            // workgroups of a launch
+
+sti_status check_cache(const sti_cache *c)
+{
+    if (!c) return STI_ERR_NULL;
+    if (c->bits != 16 && c->bits != 8 && c->bits != 4) return STI_ERR_BITWIDTH;
+    if (c->n_kv_heads < 1 || c->n_kv_heads > kMaxCacheHeads || (c->d_head != 64 && c->d_head != 128)) return STI_ERR_DIMS;
+    if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) || c->n_pages < 0) return STI_ERR_DIMS;
+    if (c->bits == 16 && c->dtype != STI_F16 && c->dtype != STI_BF16) return STI_ERR_DTYPE;
+    return STI_OK;
+}
+
+sti_status check_batch(const sti_cache &c, const sti_cache_batch *b)
+{
+    if (!b) return STI_ERR_NULL;
+    if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_pages < 0 || b->n_tokens > kMostTokens) return STI_ERR_DIMS;
+    if ((int64_t)b->max_pages * c.page_tokens > kMostPositions) return STI_ERR_DIMS;
+    return STI_OK;
+}
+
+// the arrays that a call with work to do reads
+sti_status check_arrays(const sti_cache &c, const sti_cache_batch &b, bool offsets)
+{
+    const bool held = c.n_pages > 0, paged = b.max_pages > 0;
+    if (held && (!c.k || !c.v || (c.bits < 16 && (!c.k_scale || !c.v_scale)))) return STI_ERR_NULL;
+    if (!b.lengths || (paged && !b.page_table) || (offsets && !b.offsets)) return STI_ERR_NULL;
+    if (held && (!aligned(c.k, 16) || !aligned(c.v, 16))) return STI_ERR_ALIGN;
+    if (held && c.bits < 16 && (!aligned(c.k_scale, 4) || !aligned(c.v_scale, 4))) return STI_ERR_ALIGN;
+    if (!aligned(b.lengths, 4) || !aligned(b.page_table, 4) || (offsets && !aligned(b.offsets, 4))) return STI_ERR_ALIGN;
+    return STI_OK;
+}
+
+sti_status check_rows(const void *rows, int64_t stride, int64_t width, sti_dtype type)
+{
+    if (!rows) return STI_ERR_NULL;
+    if (stride < width) return STI_ERR_DIMS;
+    const int64_t bytes = type == STI_F32 ? 4 : 2;
+    return aligned(rows, 16) && (stride * bytes) % 16 == 0 ? STI_OK : STI_ERR_ALIGN;
+}
+
+bool known(sti_dtype t) { return t == STI_F32 || t == STI_F16 || t == STI_BF16; }
+
+int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
+
+CacheView view(const sti_cache &c)
+{
+    return CacheView{(const uint8_t *)c.k, (const uint8_t *)c.v, c.k_scale, c.v_scale, c.n_kv_heads, log2_of(c.page_tokens), c.n_pages};
+}
+BatchView view(const sti_cache_batch &b) { return BatchView{b.page_table, b.lengths, b.offsets, b.n_seqs, b.n_tokens, b.max_pages}; }
+
+template <typename F>
+sti_status timed_call(int cls, F launch_it)
+{
+    const sti_status st = begin_timed(cls);
+    if (st != STI_OK) return st;
+    const hipError_t e = launch_it();
+    end_timed();
+    return e == hipSuccess ? STI_OK : STI_ERR_HIP;
+}
+
+bool valid_heads(const sti_cache &c, const sti_cache_batch &b, int32_t n_heads)
+{
+    return n_heads >= 1 && n_heads <= kMaxQueryHeads && n_heads % c.n_kv_heads == 0 && (int64_t)b.n_tokens * n_heads <= kMostPositions;
+}
+
+AttentionCut cut_of(const sti_cache &c, const sti_cache_batch &b, int32_t n_heads, int32_t window, int32_t sinks)
+{
+    return attention_cut(b.n_tokens, b.n_seqs, n_heads, c.n_kv_heads, (int64_t)b.max_pages * c.page_tokens, window, sinks);
+}
+
+}  // namespace
+
+extern "C" {
+
+sti_status sti_cache_append(const sti_cache *cache, const sti_cache_batch *batch, const void *k, const void *v, sti_dtype io_dtype,
+                            int64_t k_stride, int64_t v_stride, void *hip_stream)
+{
+    sti_status st = check_cache(cache);
+    if (st == STI_OK) st = check_batch(*cache, batch);
+    if (st != STI_OK) return st;
+    if (!known(io_dtype)) return STI_ERR_DTYPE;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return STI_OK;
+    st = check_arrays(*cache, *batch, true);
+    if (st == STI_OK) st = check_rows(k, k_stride, (int64_t)cache->n_kv_heads * cache->d_head, io_dtype);
+    if (st == STI_OK) st = check_rows(v, v_stride, (int64_t)cache->n_kv_heads * cache->d_head, io_dtype);
+    if (st != STI_OK || cache->n_pages == 0 || batch->max_pages == 0) return st;
+    return timed_call(STI_K_CONVERT, [&] {
+        return launch_cache_append(view(*cache), view(*batch), cache->bits, cache->d_head, cache->dtype, k, v, io_dtype, k_stride, v_stride,
+                                   (hipStream_t)hip_stream);
+    });
+}
+
+sti_status sti_cache_read(const sti_cache *cache, const sti_cache_batch *batch, int32_t first, int32_t count, void *k_out, void *v_out,
+                          sti_dtype out_dtype, void *hip_stream)
+{
+    sti_status st = check_cache(cache);
+    if (st == STI_OK) st = check_batch(*cache, batch);
+    if (st != STI_OK) return st;
+    if (first < 0 || count < 0 || (int64_t)first + count > kMostPositions) return STI_ERR_DIMS;
+    if (!known(out_dtype)) return STI_ERR_DTYPE;
+    if (((int64_t)count + 15) / 16 * 16 * batch->n_seqs * cache->n_kv_heads / 16 > kMostBlocks) return STI_ERR_DIMS;
+    if (batch->n_seqs == 0 || count == 0) return STI_OK;
+    st = check_arrays(*cache, *batch, false);
+    if (st != STI_OK) return st;
+    if (!k_out || !v_out) return STI_ERR_NULL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return STI_ERR_ALIGN;
+    return timed_call(STI_K_CONVERT, [&] {
+        return launch_cache_read(view(*cache), view(*batch), cache->bits, cache->d_head, cache->dtype, first, count, k_out, v_out, out_dtype,
+                                 (hipStream_t)hip_stream);
+    });
+}
+
+size_t sti_cache_attention_workspace_bytes(const sti_cache *cache, const sti_cache_batch *batch, int32_t n_heads, int32_t window,
+                                           int32_t sinks)
+{
+    if (check_cache(cache) != STI_OK || check_batch(*cache, batch) != STI_OK || !valid_heads(*cache, *batch, n_heads)) return 0;
+    if (window < 0 || sinks < 0 || batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
+    return partial_bytes(batch->n_tokens, n_heads, cache->d_head, cut_of(*cache, *batch, n_heads, window, sinks).splits);
+}
+
+sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *batch, const void *q, void *out, sti_dtype io_dtype,
+                               int64_t q_stride, int64_t out_stride, int32_t n_heads, float scale, int32_t window, int32_t sinks,
+                               void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    sti_status st = check_cache(cache);
+    if (st == STI_OK) st = check_batch(*cache, batch);
+    if (st != STI_OK) return st;
+    if (io_dtype != STI_F16 && io_dtype != STI_BF16) return STI_ERR_DTYPE;
+    if (cache->bits == 16 && cache->dtype != io_dtype) return STI_ERR_UNSUPPORTED;
+    if (!valid_heads(*cache, *batch, n_heads) || window < 0 || sinks < 0) return STI_ERR_DIMS;
+    if (!(scale >= 0.f) || !isfinite(scale)) return STI_ERR_DIMS;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return STI_OK;
+    st = check_arrays(*cache, *batch, true);
+    if (st == STI_OK) st = check_rows(q, q_stride, (int64_t)n_heads * cache->d_head, io_dtype);
+    if (st == STI_OK) st = check_rows(out, out_stride, (int64_t)n_heads * cache->d_head, io_dtype);
+    if (st != STI_OK) return st;
+    const AttentionCut cut = cut_of(*cache, *batch, n_heads, window, sinks);
+    const size_t need = partial_bytes(batch->n_tokens, n_heads, cache->d_head, cut.splits);
+    if (need && (!workspace || workspace_bytes < need)) return STI_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return STI_ERR_ALIGN;
+    if (cut.tiles * cut.splits * cache->n_kv_heads > kMostBlocks) return STI_ERR_DIMS;
+    AttentionCall a;
+    a.cache = view(*cache);
+    a.batch = view(*batch);
+    if (cache->n_pages == 0) a.batch.max_pages = 0;   // nothing is held: no key is seen
+    a.bits = cache->bits;
+    a.d = cache->d_head;
+    a.heads = n_heads;
+    a.group = n_heads / cache->n_kv_heads;
+    a.bf16 = io_dtype == STI_BF16;
+    a.scale = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->d_head)) * 1.44269504088896340736f;
+    a.window = (int32_t)std::min<int64_t>(window, kMostPositions);
+    a.sinks = (int32_t)std::min<int64_t>(sinks, kMostPositions);
+    a.q = q;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    st = timed_call(STI_K_ATTENTION, [&] { return launch_cache_attention(a, cut, (float *)workspace, (hipStream_t)hip_stream); });
+    if (st != STI_OK || cut.splits == 1) return st;
+    return timed_call(STI_K_ATTENTION, [&] { return launch_cache_join(a, cut.splits, (const float *)workspace, (hipStream_t)hip_stream); });
+}
+
+}  // extern "C"
