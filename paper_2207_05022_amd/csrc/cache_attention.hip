@@ -287,7 +287,7 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     // rows that share a key/value head in an average sequence
     const int64_t rows = (n_tokens + n_seqs - 1) / n_seqs * group;
     AttentionCut cut;
-    cut.tile_rows = rows <= 1 ? 1 : rows <= 2 ? 2 : 4;
+    cut.tile_rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     cut.tiles = tile_bound(n_tokens, n_seqs, group, cut.tile_rows);
     int64_t keys = capacity;   // the most that a tile's queries see (its tokens: at most tile_rows of them)
     if (window > 0) keys = std::min(keys, (int64_t)window + sinks + cut.tile_rows);
@@ -299,6 +299,7 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
 
 hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
 {
+    if (cut.tile_rows > 4) return launch_cache_tiles(a, cut, partials, stream);
     if (a.d == 64)
         a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);
     else

@@ -1,0 +1,504 @@
+// Attention of many queries per sequence over a paged cache, on the matrix cores.
+//
+// Tiles of 32 WR queries of one key/value head; WK groups of WR waves walk the tile's keys KT at a time, each group its own steps.  Everything
+// is computed transposed, as in attention_core.hpp: S^T = K Q^T leaves a lane one query and 16 keys per 32, O^T = V^T P^T takes the weights in
+// the registers where they are, and the maximum of a query crosses only lanes l and l ^ 32.
+//
+//   t_j = c s_k[j] (q . code_k[j]) + log2 s_v[j],   P_j = 2^(t_j - m),   o = sum_j P_j code_v[j] / sum_j P_j / s_v[j]
+//
+// with codes (16 bits: s_k = s_v = 1): codes are exact in 16 bits, so that the only rounding in front of the matrix cores is that of the
+// weights, and a value's scale takes part in the maximum, so that a weight is largest where the value it carries is.  (The scale in the
+// value instead: another rounding per value; beside the weight without the maximum: weights of small values below 2^-14, the normal numbers of
+// binary16.)  Keys and values of a step go through registers to LDS (codes become 16-bit numbers on the way), one step ahead of the products;
+// V^T is read from its rows by the transposing LDS read.
+#include "cache_common.hpp"
+
+namespace sti {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+template <bool BF>
+__device__ inline float16v product(u32x4 a, u32x4 b, float16v c)
+{
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+template <bool BF>
+__device__ inline float number(uint32_t half)
+{
+    if constexpr (BF) return __builtin_bit_cast(float, half << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)half);
+}
+template <bool BF>
+__device__ inline uint32_t pair_bits(float lo, float hi)   // rounded to nearest even
+{
+    if constexpr (BF) {
+        const bf16x2 h = {(__bf16)lo, (__bf16)hi};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+    return f16_pair_bits(lo, hi);
+}
+
+// Codes -> numbers of the matrix cores' type, exactly.  Binary16: a byte under 0x64 is 1024 + byte; bfloat16: through float32.
+__device__ inline uint32_t less(uint32_t pair, uint32_t by)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, pair) - __builtin_bit_cast(half2v, by));
+}
+template <bool BF>
+__device__ inline u32x4 numbers_of_bytes(uint32_t w0, uint32_t w1)   // 8 codes of 8 bits
+{
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? w0 : w1;
+        const int at = 16 * (i & 1);
+        if constexpr (BF) {
+            const float lo = (float)(int8_t)(w >> at), hi = (float)(int8_t)(w >> (at + 8));
+            out[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+        } else {
+            const uint32_t u = w ^ 0x80808080u;
+            out[i] = less(__builtin_amdgcn_perm(0x64646464u, u, i & 1 ? 0x04030402u : 0x04010400u), 0x64806480u);   // 1024 + 128
+        }
+    }
+    return out;
+}
+template <bool BF>
+__device__ inline u32x4 numbers_of_nibbles(uint32_t w)   // 8 codes of 4 bits
+{
+    const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF) {
+            const float lo = (float)((int)(even >> (8 * i) & 15) - 8), hi = (float)((int)(odd >> (8 * i) & 15) - 8);
+            out[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+        } else {
+            const uint32_t pair = __builtin_amdgcn_perm(odd, even, 0x0C040C00u + 0x00010001u * i) | 0x64006400u;
+            out[i] = less(pair, 0x64086408u);   // 1024 + 8
+        }
+    }
+    return out;
+}
+
+// Values that are not finite numbers (16 bits): 0 times one is not 0, so that in steps that not every query sees they are kept from the
+// matrix cores and added to the results of the queries that see them (a weight other than 1 would not change what comes of it).
+template <bool BF>
+__device__ inline uint32_t odd_halves(uint32_t pair)   // all bits of the halves whose exponent is the largest
+{
+    constexpr uint32_t kLow = BF ? 0x7F80u : 0x7C00u, kHigh = kLow << 16;
+    return ((pair & kLow) == kLow ? 0xFFFFu : 0u) | ((pair & kHigh) == kHigh ? 0xFFFF0000u : 0u);
+}
+template <bool BF>
+__device__ inline u32x4 without_odd(u32x4 v)
+{
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = v[i] & ~odd_halves<BF>(v[i]);
+    return out;
+}
+
+template <int BITS, int D, int WR, int WK>
+struct TileShape {
+    static constexpr int KT = WR == 4 ? 64 : 32;         // keys of a step
+    static constexpr int BUFFERS = WR == 1 ? 1 : 2;      // a wave that has its step to itself writes behind its own reads
+    static constexpr int THREADS = 64 * WR;              // of a group
+    static constexpr int KS = D + 8, VS = D + 32;        // halves per row in LDS: no two lanes of a read share a bank
+    static constexpr int CHUNK = BITS == 16 ? 8 : 16;    // values of a request: 16 bytes, 8 of codes of 4 bits
+    static constexpr int ROW_CHUNKS = D / CHUNK, ITEMS = KT * ROW_CHUNKS / THREADS;
+    static constexpr int STEP_HALVES = KT * (KS + VS), SCALES = BITS < 16 ? 3 * KT : 0;
+    static constexpr int STEP_BYTES = STEP_HALVES * 2 + SCALES * 4;
+    static constexpr int JOIN_FLOATS = WK > 1 ? WK * 32 * WR * (D + 4) : 0;   // results of the groups, at the end
+    static constexpr int STAGE_BYTES = STEP_BYTES * BUFFERS * WK;
+    static constexpr int LDS_BYTES = STAGE_BYTES > JOIN_FLOATS * 4 ? STAGE_BYTES : JOIN_FLOATS * 4;
+    static_assert(WR * WK == 4 && KT * ROW_CHUNKS % THREADS == 0, "");
+};
+
+template <int BITS, bool BF, int D, int WR, int WK>
+__global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, uint32_t group_recip, uint32_t tiles_recip, uint32_t splits_recip, int tiles,
+                                                             int splits, int pieces, int per_xcd, float *partials)
+{
+    using T = TileShape<BITS, D, WR, WK>;
+    constexpr int KT = T::KT, KS = T::KS, VS = T::VS, ROWS = 32 * WR, NKB = KT / 32, ROW_BYTES = D * BITS / 8, CHUNK_BYTES = T::CHUNK * BITS / 8;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[T::LDS_BYTES];
+    __shared__ float tops[WK][ROWS], weights[WK][ROWS];
+    __shared__ int odd_step[WK][T::BUFFERS];   // the last step whose values, where some query may not see them, are not all finite
+    const CacheView &c = a.cache;
+    const BatchView &b = a.batch;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
+    const int g = lane >> 5, lr = lane & 31, tid = wr * 64 + lane;   // (tid: inside the group)
+    const int piece = piece_of_block(blockIdx.x, per_xcd);
+    if (piece >= pieces) return;
+    // (head, split, tile): the tiles of a head, which read the same keys, lie behind each other and go to one XCD
+    const int head_split = quotient(piece, tiles, tiles_recip), tile = piece - head_split * tiles;
+    const int head = quotient(head_split, splits, splits_recip), split = head_split - head * splits;
+    const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
+    if (t.seq < 0) return;
+
+    // this lane's query as the B operand of S^T = K Q^T
+    const int row = t.row0 + min(wr * 32 + lr, t.rows - 1), token = quotient(row, a.group, group_recip);
+    const int pos = t.base + token, q_head = head * a.group + row - token * a.group;
+    const bool idle = wr * 32 >= t.rows;
+    const int wave_last = t.row0 + min(wr * 32 + 31, t.rows - 1);
+    const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, group_recip), last_pos = t.base + quotient(wave_last, a.group, group_recip);
+    u32x4 qf[D / 16];
+    {
+        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * 8;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + s * 16);
+    }
+
+    const int steps = (t.keys.count + KT - 1) / KT, share = (steps + splits - 1) / splits;
+    const int step0 = split * share, step1 = min(steps, step0 + share);
+    const int x_end = min(t.keys.count, step1 * KT);
+    const int rounds = max(0, (step1 - step0 + WK - 1) / WK);   // the same for all groups: they meet at barriers
+
+    const int x_first = (step0 + wk) * KT, x_stride = WK * KT;   // the group's steps
+
+    float16v o[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[e][v] = 0.f;
+    float top = -INFINITY, sum = 0.f;   // (16 bits: top in units of the unscaled scores; sum: of this lane's keys)
+
+    // one step on its way: raw rows in registers, pages of the one behind it
+    u32x4 kr[T::ITEMS], vr[T::ITEMS];
+    float scale_k = 0.f, scale_v = 0.f;
+    int pages = -1, pages_now = -1;   // of key `lane` % KT of a step
+    auto ask_pages = [&](int x0) {
+        const int x = x0 + (lane & (KT - 1));
+        if (x0 < x_end) pages = cache_page(c, b, t.seq, t.keys.key(min(x, x_end - 1)));
+    };
+    auto ask_rows = [&](int x0) {
+        if (x0 >= x_end) return;
+#pragma unroll
+        for (int i = 0; i < T::ITEMS; ++i) {
+            const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, part = item % T::ROW_CHUNKS;
+            const int page = max(__shfl(pages, r), 0);
+            const int64_t at = cache_row(c, page, head, t.keys.key(min(x0 + r, x_end - 1))) * ROW_BYTES + part * CHUNK_BYTES;
+            if constexpr (BITS == 4) {
+                const u32x2 k2 = *(const u32x2 *)(c.k + at), v2 = *(const u32x2 *)(c.v + at);
+                kr[i] = u32x4{k2.x, k2.y, 0, 0};
+                vr[i] = u32x4{v2.x, v2.y, 0, 0};
+            } else {
+                kr[i] = *(const u32x4 *)(c.k + at);
+                vr[i] = *(const u32x4 *)(c.v + at);
+            }
+        }
+        if constexpr (BITS < 16) {
+            const int64_t at = cache_row(c, max(pages, 0), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));
+            scale_k = c.k_scale[at];
+            scale_v = c.v_scale[at];
+        }
+    };
+    auto step_lds = [&](int buffer) { return lds + (wk * T::BUFFERS + buffer) * T::STEP_BYTES; };
+    auto put_rows = [&](int buffer, int n, int of_pages) {   // n: the step's number inside the group
+        if (BITS == 16) {
+            const int x0 = x_first + n * x_stride;
+            const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
+            const bool seen_by_all = x0 + KT <= x_end && key_last <= t.first_pos && (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);
+            if (!seen_by_all || __any(of_pages < 0)) {
+                uint32_t odd = 0;
+#pragma unroll
+                for (int i = 0; i < T::ITEMS; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) odd |= odd_halves<BF>(vr[i][j]);
+                if (odd) odd_step[wk][buffer] = n;
+            }
+        }
+        uint16_t *ks = (uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
+#pragma unroll
+        for (int i = 0; i < T::ITEMS; ++i) {
+            const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, at = item % T::ROW_CHUNKS * T::CHUNK;
+            u32x4 *kd = (u32x4 *)(ks + r * KS + at), *vd = (u32x4 *)(vs + r * VS + at);
+            if constexpr (BITS == 16) {
+                kd[0] = kr[i];
+                vd[0] = vr[i];
+            } else if constexpr (BITS == 8) {
+                kd[0] = numbers_of_bytes<BF>(kr[i][0], kr[i][1]);
+                kd[1] = numbers_of_bytes<BF>(kr[i][2], kr[i][3]);
+                vd[0] = numbers_of_bytes<BF>(vr[i][0], vr[i][1]);
+                vd[1] = numbers_of_bytes<BF>(vr[i][2], vr[i][3]);
+            } else {
+                kd[0] = numbers_of_nibbles<BF>(kr[i][0]);
+                kd[1] = numbers_of_nibbles<BF>(kr[i][1]);
+                vd[0] = numbers_of_nibbles<BF>(vr[i][0]);
+                vd[1] = numbers_of_nibbles<BF>(vr[i][1]);
+            }
+        }
+        if constexpr (BITS < 16) {
+            float *sc = (float *)(vs + KT * VS);
+            if (tid < KT) {
+                // a row of zeros has scale 0: any small one serves, its weight counts in the sum alone
+                const float s = scale_v == 0.f ? 0x1p-100f : scale_v;
+                sc[tid] = scale_k * a.scale;
+                sc[KT + tid] = __builtin_amdgcn_logf(s);   // log2
+                sc[2 * KT + tid] = 1.0f / s;
+            }
+        }
+    };
+    auto meet = [&]() {
+        if constexpr (WR == 1)
+            wave_lds_fence();
+        else
+            __syncthreads();
+    };
+
+    if (lane == 0)
+        for (int i = 0; i < T::BUFFERS; ++i) odd_step[wk][i] = -1;   // (the waves of a group write the same; a find comes behind the barrier)
+    meet();
+    ask_pages(x_first);
+    ask_rows(x_first);
+    pages_now = pages;
+    ask_pages(x_first + x_stride);
+    put_rows(0, 0, pages_now);
+    meet();
+    for (int n = 0; n < rounds; ++n) {
+        const int x0 = x_first + n * x_stride, buffer = T::BUFFERS == 2 ? n & 1 : 0;
+        ask_rows(x0 + x_stride);
+        const int pages_next = pages;
+        ask_pages(x0 + 2 * x_stride);
+        const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
+        const bool none = idle || x0 >= x_end || key_first > last_pos || (a.window > 0 && key_first >= a.sinks && key_last <= first_pos - a.window);
+        if (!none) {
+            const uint16_t *ks = (const uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
+            const float *sc = (const float *)(vs + KT * VS);
+            const uint64_t held = __ballot(pages_now >= 0);   // bit j: the page of key j is there (KT 32: bits twice)
+            const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
+                               (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);
+            float16v s[NKB];
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    s[kb] = product<BF>(*(const u32x4 *)(ks + (kb * 32 + lr) * KS + i * 16 + g * 8), qf[i], s[kb]);
+            }
+            uint32_t seen[NKB];   // bit v: this lane's query sees the key of register v
+            if constexpr (BITS < 16) {
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4) {
+                        const float4v k4 = *(const float4v *)(sc + kb * 32 + v4 * 8 + g * 4), l4 = *(const float4v *)(sc + KT + kb * 32 + v4 * 8 + g * 4);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) s[kb][v4 * 4 + v] = fmaf(s[kb][v4 * 4 + v], k4[v], l4[v]);
+                    }
+            }
+            if (!plain) {
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb) {
+                    seen[kb] = 0;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int j = kb * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
+                        const bool see = x0 + j < x_end && (held >> j & 1) && sees(pos, t.keys.key(x0 + j), a.window, a.sinks);
+                        seen[kb] |= see ? 1u << v : 0u;
+                        s[kb][v] = see ? s[kb][v] : -INFINITY;
+                    }
+                }
+            }
+            float m = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) m = fmaxf(m, s[kb][v]);
+            m = pair_max(across_32(m));
+            // A query's results are shrunk only where its maximum has grown by more than 2^8: weights up to 256 are as exact as those up to 1.
+            const float scale = BITS == 16 ? a.scale : 1.f;
+            const bool grown = (m - top) * scale > 8.f || (top == -INFINITY && m > -INFINITY);
+            if (__any(grown)) {
+                const float f = grown ? __builtin_amdgcn_exp2f((top - m) * scale) : 1.f;
+                top = grown ? m : top;
+                sum *= f;
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[e][v] *= f;
+            }
+            const bool odd = BITS == 16 && !plain && uniform(odd_step[wk][buffer]) == n;
+            if (odd) {
+                for (int j = 0; j < KT; ++j) {
+                    const bool see = x0 + j < x_end && (held >> j & 1) && sees(pos, t.keys.key(x0 + j), a.window, a.sinks);
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                        for (int v4 = 0; v4 < 4; ++v4) {
+                            const u32x2 w = *(const u32x2 *)(vs + j * VS + e * 32 + v4 * 8 + g * 4);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
+                                if (bad & 1) o[e][v4 * 4 + 2 * i] += number<BF>(pair & 0xFFFFu);
+                                if (bad >> 31) o[e][v4 * 4 + 2 * i + 1] += number<BF>(pair >> 16);
+                            }
+                        }
+                }
+            }
+            const float shift = top == -INFINITY ? 0.f : -top * scale;
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+                uint32_t pk[8];
+#pragma unroll
+                for (int v4 = 0; v4 < 4; ++v4) {
+                    float p[4];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) p[v] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(s[kb][v4 * 4 + v], scale, shift) : s[kb][v4 * 4 + v] + shift);
+                    if constexpr (BITS == 16) {
+                        sum += (p[0] + p[1]) + (p[2] + p[3]);
+                    } else {
+                        const float4v i4 = *(const float4v *)(sc + 2 * KT + kb * 32 + v4 * 8 + g * 4);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const float w = fmaf(p[v], i4[v], sum);
+                            sum = plain || (seen[kb] >> (v4 * 4 + v) & 1) ? w : sum;   // (a scale that is not seen may be NaN)
+                        }
+                    }
+                    pk[v4 * 2] = pair_bits<BF>(p[0], p[1]);
+                    pk[v4 * 2 + 1] = pair_bits<BF>(p[2], p[3]);
+                }
+                // O^T += V^T P^T, 16 keys at a time in the order of the registers
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const u32x4 pf = {pk[4 * h], pk[4 * h + 1], pk[4 * h + 2], pk[4 * h + 3]};
+                    const uint16_t *vrow = vs + (kb * 32 + h * 16 + g * 4 + ((lane & 15) >> 2)) * VS + (lane & 16) + (lane & 3) * 4;
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e) {
+                        typedef __attribute__((address_space(3))) short4v *LdsShort4;
+                        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + e * 32)));
+                        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + 8 * VS + e * 32)));
+                        u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
+                        if (BITS == 16 && odd) vf = without_odd<BF>(vf);
+                        o[e] = product<BF>(vf, pf, o[e]);
+                    }
+                }
+            }
+        }
+        if constexpr (T::BUFFERS == 1) meet();
+        put_rows(T::BUFFERS == 2 ? (n + 1) & 1 : 0, n + 1, pages_next);
+        meet();
+        pages_now = pages_next;
+    }
+
+    sum = pair_sum(across_32(sum));
+    if constexpr (BITS == 16) top = top == -INFINITY ? top : top * a.scale;
+    const int64_t line = (int64_t)b.n_tokens * a.heads, plane = (int64_t)split * line;
+    if constexpr (WK == 1) {
+        if (wr * 32 + lr >= t.rows) return;
+        const int64_t to_row = (int64_t)(t.first + token);
+        if (splits == 1) {
+            const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+            uint16_t *out = (uint16_t *)a.out + to_row * a.out_stride + q_head * D + g * 4;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                for (int v4 = 0; v4 < 4; ++v4) {
+                    const u32x2 w = {pair_bits<BF>(o[e][v4 * 4] * inv, o[e][v4 * 4 + 1] * inv), pair_bits<BF>(o[e][v4 * 4 + 2] * inv, o[e][v4 * 4 + 3] * inv)};
+                    *(u32x2 *)(out + e * 32 + v4 * 8) = w;
+                }
+        } else {
+            const int64_t at = plane + to_row * a.heads + q_head;
+            float *out = partials + at * D + g * 4;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(out + e * 32 + v4 * 8) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
+            if (g == 0) {
+                float *ml = partials + (int64_t)splits * line * D + at * 2;
+                ml[0] = top;
+                ml[1] = sum;
+            }
+        }
+    } else {
+        // the groups' results, over the staged steps
+        __syncthreads();
+        float *join = (float *)lds;
+        constexpr int JS = D + 4;
+        float *mine = join + (wk * ROWS + wr * 32 + lr) * JS + g * 4;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(mine + e * 32 + v4 * 8) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
+        if (g == 0) {
+            tops[wk][wr * 32 + lr] = top;
+            weights[wk][wr * 32 + lr] = sum;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < t.rows * (D / 4); i += 256) {
+            const int r = i / (D / 4), at = i % (D / 4) * 4;
+            float m = tops[0][r], l = 0.f;
+#pragma unroll
+            for (int w = 1; w < WK; ++w) m = fmaxf(m, tops[w][r]);
+            float4v v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float f = tops[w][r] == m ? 1.f : __builtin_amdgcn_exp2f(tops[w][r] - m);
+                const float4v x = *(const float4v *)(join + (w * ROWS + r) * JS + at);
+                l += weights[w][r] * f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += x[j] * f;
+            }
+            const int rr = t.row0 + r, tok = quotient(rr, a.group, group_recip), qh = head * a.group + rr - tok * a.group;
+            if (splits == 1) {
+                const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+                const u32x2 w = {pair_bits<BF>(v[0] * inv, v[1] * inv), pair_bits<BF>(v[2] * inv, v[3] * inv)};
+                *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + at) = w;
+            } else {
+                const int64_t to = plane + (int64_t)(t.first + tok) * a.heads + qh;
+                *(float4v *)(partials + to * D + at) = v;
+                if (at == 0) {
+                    float *ml = partials + (int64_t)splits * line * D + to * 2;
+                    ml[0] = m;
+                    ml[1] = l;
+                }
+            }
+        }
+    }
+}
+
+template <int BITS, bool BF, int D>
+void launch_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    const int pieces = (int)(cut.tiles * cut.splits * a.cache.heads), per_xcd = pieces_per_xcd(pieces);
+    const dim3 grid((uint32_t)(per_xcd * 8));
+    const uint32_t gr = reciprocal((uint32_t)a.group), tr = reciprocal((uint32_t)cut.tiles), sr = reciprocal((uint32_t)cut.splits);
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, tr, sr, (int)cut.tiles, cut.splits, pieces, per_xcd, partials); };
+    if (cut.tile_rows == 32)
+        go(cache_tiles_kernel<BITS, BF, D, 1, 4>);
+    else if (cut.tile_rows == 64)
+        go(cache_tiles_kernel<BITS, BF, D, 2, 2>);
+    else
+        go(cache_tiles_kernel<BITS, BF, D, 4, 1>);
+}
+template <bool BF, int D>
+void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    if (a.bits == 16)
+        launch_tiles<16, BF, D>(a, cut, partials, stream);
+    else if (a.bits == 8)
+        launch_tiles<8, BF, D>(a, cut, partials, stream);
+    else
+        launch_tiles<4, BF, D>(a, cut, partials, stream);
+}
+
+}  // namespace
+
+hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    if (a.d == 64)
+        a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);
+    else
+        a.bf16 ? launch_bits<true, 128>(a, cut, partials, stream) : launch_bits<false, 128>(a, cut, partials, stream);
+    return hipGetLastError();
+}
+
+}  // namespace sti

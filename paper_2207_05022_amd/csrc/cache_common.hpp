@@ -146,6 +146,7 @@ inline size_t partial_bytes(int64_t n_tokens, int heads, int d, int splits)
     return splits > 1 ? (size_t)splits * n_tokens * heads * (d + 2) * sizeof(float) : 0;
 }
 hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);
+hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);   // tile_rows 32 and more
 hipError_t launch_cache_join(const AttentionCall &a, int splits, const float *partials, hipStream_t stream);
 
 }  // namespace sti
