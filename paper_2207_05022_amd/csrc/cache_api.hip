@@ -9,6 +9,7 @@ namespace {
 
 constexpr int64_t kMostPositions = (int64_t)1 << 30;   // of a sequence: sums and differences of positions and windows fit 32 bits
 constexpr int64_t kMostTokens = (int64_t)1 << 24;      // new tokens of a call
+constexpr int64_t kMostRows = (int64_t)1 << 32;        // of a pool
 constexpr int64_t kMostBlocks = 0x7FFFFFFF;            // workgroups of a launch
 
 sti_status check_cache(const sti_cache *c)
@@ -17,6 +18,7 @@ sti_status check_cache(const sti_cache *c)
     if (c->bits != 16 && c->bits != 8 && c->bits != 4) return STI_ERR_BITWIDTH;
     if (c->n_kv_heads < 1 || c->n_kv_heads > kMaxCacheHeads || (c->d_head != 64 && c->d_head != 128)) return STI_ERR_DIMS;
     if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) || c->n_pages < 0) return STI_ERR_DIMS;
+    if ((int64_t)c->n_pages * c->page_tokens * c->n_kv_heads >= kMostRows) return STI_ERR_DIMS;
     if (c->bits == 16 && c->dtype != STI_F16 && c->dtype != STI_BF16) return STI_ERR_DTYPE;
     return STI_OK;
 }

@@ -6,13 +6,15 @@
 // asks for 64 / LPK rows at once and the values arrive as they lie: no transposition, no LDS.  A group of LPK lanes keeps a running maximum, sum
 // and result of its own keys; groups and waves are joined once, at the end, and so are the splits of a long sequence over workgroups
 // (cache_join_kernel).  All arithmetic is float32 on values or codes as they are stored; a row's scale multiplies its score and its weight.
-#include "cache_common.hpp"
+#include "cache_numbers.hpp"
 
 namespace sti {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef cache_u32x4 u32x4;
+typedef cache_u32x2 u32x2;
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
 
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
             const int page = cache_page(c, b, t.seq, key[u]);
             there[u] = x < x_end && page >= 0;
             plain &= page >= 0;
-            const int64_t row = cache_row(c, max(page, 0), head, key[u]);
+            const int64_t row = (int64_t)cache_row(c, max(page, 0), head, key[u]);
             k[u].load(c.k + row * ROW_BYTES + part * P::BYTES);
             v[u].load(c.v + row * ROW_BYTES + part * P::BYTES);
             if constexpr (BITS < 16) {
@@ -233,27 +235,56 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
     }
 }
 
-// One (token, head) row per D threads: the splits' results, each shrunk to the largest maximum.
-template <bool BF, int D>
+// The splits' results, each shrunk to the largest maximum.  D / 4 threads of 4 features take a row's splits GROUPS at a time; the groups of a row
+// are joined through LDS.
+template <bool BF, int D, int GROUPS>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32_t heads_recip, int splits, const float *partials)
 {
+    constexpr int WIDE = D / 4, PER_ROW = WIDE * GROUPS, ROWS = 256 / PER_ROW;
+    __shared__ float4v sums[GROUPS > 1 ? GROUPS : 1][WIDE];
+    __shared__ float tops[GROUPS], weights[GROUPS];
     const BatchView &b = a.batch;
     const int64_t line = (int64_t)b.n_tokens * a.heads;
-    const int row = (int)(blockIdx.x * (256 / D) + threadIdx.x / D), at = threadIdx.x % D;
-    if (row >= line) return;
+    const int row = (int)(blockIdx.x * ROWS + threadIdx.x / PER_ROW), group = threadIdx.x / WIDE % GROUPS, at = threadIdx.x % WIDE;
+    if (row >= line) return;   // (whole blocks where groups meet)
     const int token = quotient(row, a.heads, heads_recip), head = row - token * a.heads;
-    if (token < b.offsets[0] || token >= b.offsets[b.n_seqs]) return;   // (of no sequence: no tile has left anything)
-    const float *ml = partials + (int64_t)splits * line * D;
-    float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[((int64_t)s * line + row) * 2]);
-    float l = 0.f, w = 0.f;
-    for (int s = 0; s < splits; ++s) {
+    const int first = b.offsets[0], end = b.offsets[b.n_seqs];
+    const float2v *ml = (const float2v *)(partials + (int64_t)splits * line * D);
+    float m = -INFINITY, l = 0.f;
+    float4v w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = group; s < splits; s += GROUPS) {
         const int64_t plane = (int64_t)s * line + row;
-        const float f = factor(ml[plane * 2], m);
-        l += ml[plane * 2 + 1] * f;
-        w += partials[plane * D + at] * f;
+        const float2v theirs = ml[plane];
+        const float4v x = *(const float4v *)(partials + plane * D + at * 4);
+        const float t = fmaxf(m, theirs.x), f0 = factor(m, t), f1 = factor(theirs.x, t);
+        m = t;
+        l = l * f0 + theirs.y * f1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = w[i] * f0 + x[i] * f1;
     }
-    ((uint16_t *)a.out)[token * a.out_stride + head * D + at] = rounded<BF>(l > 0.f ? w / l : (l == 0.f ? 0.f : l));
+    if constexpr (GROUPS > 1) {
+        sums[group][at] = w;
+        if (at == 0) {
+            tops[group] = m;
+            weights[group] = l;
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int j = 1; j < GROUPS; ++j) {
+            const float theirs = tops[j], t = fmaxf(m, theirs), f0 = factor(m, t), f1 = factor(theirs, t);
+            const float4v x = sums[j][at];
+            m = t;
+            l = l * f0 + weights[j] * f1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = w[i] * f0 + x[i] * f1;
+        }
+    }
+    if (token < first || token >= end) return;   // (of no sequence: no tile has left anything)
+    const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+    const u32x2 out = {cache_pair<BF>(w[0] * inv, w[1] * inv), cache_pair<BF>(w[2] * inv, w[3] * inv)};
+    *(u32x2 *)((uint16_t *)a.out + token * a.out_stride + head * D + at * 4) = out;
 }
 
 template <int BITS, bool BF, int D>
@@ -261,12 +292,7 @@ void launch_rows(const AttentionCall &a, const AttentionCut &cut, float *partial
 {
     const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
     const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    if (cut.tile_rows == 1)
-        launch(cache_attention_kernel<BITS, BF, D, 1>, grid, dim3(kWaves * 64), 0, stream, a, gr, hr, sr, cut.splits, partials);
-    else if (cut.tile_rows == 2)
-        launch(cache_attention_kernel<BITS, BF, D, 2>, grid, dim3(kWaves * 64), 0, stream, a, gr, hr, sr, cut.splits, partials);
-    else
-        launch(cache_attention_kernel<BITS, BF, D, 4>, grid, dim3(kWaves * 64), 0, stream, a, gr, hr, sr, cut.splits, partials);
+    launch(cache_attention_kernel<BITS, BF, D, 1>, grid, dim3(kWaves * 64), 0, stream, a, gr, hr, sr, cut.splits, partials);
 }
 template <bool BF, int D>
 void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
@@ -287,7 +313,7 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     // rows that share a key/value head in an average sequence
     const int64_t rows = (n_tokens + n_seqs - 1) / n_seqs * group;
     AttentionCut cut;
-    cut.tile_rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    cut.tile_rows = rows <= 1 ? 1 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     cut.tiles = tile_bound(n_tokens, n_seqs, group, cut.tile_rows);
     int64_t keys = capacity;   // the most that a tile's queries see (its tokens: at most tile_rows of them)
     if (window > 0) keys = std::min(keys, (int64_t)window + sinks + cut.tile_rows);
@@ -299,7 +325,8 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
 
 hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
 {
-    if (cut.tile_rows > 4) return launch_cache_tiles(a, cut, partials, stream);
+    if (cut.tile_rows > 32) return launch_cache_tiles(a, cut, partials, stream);
+    if (cut.tile_rows > 1) return launch_cache_few(a, cut, partials, stream);
     if (a.d == 64)
         a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);
     else
@@ -310,14 +337,23 @@ hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cu
 hipError_t launch_cache_join(const AttentionCall &a, int splits, const float *partials, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.batch.n_tokens * a.heads;
-    const dim3 grid((uint32_t)((rows * a.d + 255) / 256));
     const uint32_t recip = reciprocal((uint32_t)a.heads);
-    if (a.d == 64)
-        a.bf16 ? launch(cache_join_kernel<true, 64>, grid, dim3(256), 0, stream, a, recip, splits, partials)
-               : launch(cache_join_kernel<false, 64>, grid, dim3(256), 0, stream, a, recip, splits, partials);
-    else
-        a.bf16 ? launch(cache_join_kernel<true, 128>, grid, dim3(256), 0, stream, a, recip, splits, partials)
-               : launch(cache_join_kernel<false, 128>, grid, dim3(256), 0, stream, a, recip, splits, partials);
+    // few splits: a row to D / 4 threads; many (few rows, then): a row to a workgroup
+    const bool many = splits > 4;
+    const int64_t threads = many ? 256 : a.d / 4;
+    const dim3 grid((uint32_t)((rows * threads + 255) / 256));
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, recip, splits, partials); };
+    if (a.d == 64) {
+        if (a.bf16)
+            many ? go(cache_join_kernel<true, 64, 16>) : go(cache_join_kernel<true, 64, 1>);
+        else
+            many ? go(cache_join_kernel<false, 64, 16>) : go(cache_join_kernel<false, 64, 1>);
+    } else {
+        if (a.bf16)
+            many ? go(cache_join_kernel<true, 128, 8>) : go(cache_join_kernel<true, 128, 1>);
+        else
+            many ? go(cache_join_kernel<false, 128, 8>) : go(cache_join_kernel<false, 128, 1>);
+    }
     return hipGetLastError();
 }
 

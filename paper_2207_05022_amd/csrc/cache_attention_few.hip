@@ -1,0 +1,417 @@
+// Attention of up to 32 queries that share keys over a paged cache, on the matrix cores: single tokens, drafts of a few, groups of heads
+// on one key/value head.
+//
+//   t_j = c s_k[j] (q . code_k[j]) + log2 s_v[j],   P_j = 2^(t_j - m),   o = sum_j P_j code_v[j] / sum_j P_j / s_v[j]
+//
+// (16 bits: s_k = s_v = 1).  Codes are exact in 16 bits, so that the only rounding in front of the matrix cores is that of the weights, and a
+// value's scale takes part in the maximum, so that a weight is largest where the value it carries is.
+//
+// A wave walks the keys KT at a time by itself, 16 queries in the columns of the products: S^T = K Q^T takes a key's row from memory as it lies,
+// a quarter of it to each group of 16 lanes (the queries' features in the same order), O^T = V^T P^T takes the weights from the registers of
+// S^T; only the values go through LDS, as stored, to be read transposed by the LDS reads for 16, 8 and 4 bits.  The maximum and the sum of a query
+// are per lane, over its 4 lanes at the end of a step.  What is asked for in a step is used in the next; waves hide what is left of the way.
+#include "cache_numbers.hpp"
+
+namespace sti {
+namespace {
+
+typedef cache_u32x4 u32x4;
+typedef cache_u32x2 u32x2;
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef int int2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+template <bool BF>
+__device__ inline float4v product(u32x4 a, u32x4 b, float4v c)
+{
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+__device__ inline float four_max(float v) { return pair_max(across_32(pair_max(across_16(v)))); }
+__device__ inline float four_sum(float v) { return pair_sum(across_32(pair_sum(across_16(v)))); }
+
+template <int BITS, int D, int NQ, int W>
+struct FewShape {
+    static constexpr int KT = BITS == 4 ? 64 : 32, NKB = KT / 16;        // keys of a step, blocks of 16 of them
+    static constexpr int ROW = D * BITS / 8;                              // bytes of a row
+    static constexpr int PIECE = ROW / 4 < 16 ? ROW / 4 : 16;            // bytes of a request: 16, or a quarter of a short row
+    static constexpr int KP = ROW / 4 / PIECE;                            // requests of a lane per key
+    static constexpr int VP = KT * ROW / PIECE / 64;                      // and for a step's values
+    static constexpr int VALUES = PIECE * 8 / BITS;                       // of a request
+    static constexpr int VS = ROW + 16;                                   // bytes per row in LDS: no two lanes of a read share a bank
+    static constexpr int STAGE = KT * VS + (BITS < 16 ? 3 * KT * 4 : 0);
+    static constexpr int JS = D + 4, HALF = W > 1 ? W / 2 : 1;
+    static constexpr int JOIN = HALF * 16 * NQ * JS * 4;
+    static constexpr int LDS = W * STAGE > JOIN ? W * STAGE : JOIN;
+};
+
+// ROWS = 16 NQ queries of one key/value head, W waves
+template <int BITS, bool BF, int D, int NQ, int W>
+__global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int splits,
+                                                              float *partials)
+{
+    using T = FewShape<BITS, D, NQ, W>;
+    constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16 * NQ, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
+    constexpr bool MBF = BITS == 16 && BF;   // the products' type
+    __shared__ __attribute__((aligned(16))) unsigned char lds[T::LDS];
+    __shared__ float tops[T::HALF][ROWS], weights[T::HALF][ROWS];
+    const CacheView &c = a.cache;
+    const BatchView &b = a.batch;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, lq = lane & 15;
+    // blocks in the order (tile, split, head)
+    const int tile_split = quotient(blockIdx.x, c.heads, heads_recip), head = blockIdx.x - tile_split * c.heads;
+    const int tile = quotient(tile_split, splits, splits_recip), split = tile_split - tile * splits;
+    const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
+    if (t.seq < 0) return;
+
+    const int steps = (t.keys.count + KT - 1) / KT, share = (steps + splits - 1) / splits;
+    const int x_end = min(t.keys.count, (split + 1) * share * KT), x_stride = W * KT;
+    int x0 = (split * share + wave) * KT;
+
+    // row of key `lane` % KT of a step in the pool, and whether its page is there
+    int page = -1;
+    uint32_t row = 0;
+    uint64_t held = 0;
+    auto key_of = [&](int x) { return t.keys.key(min(x + (lane & (KT - 1)), x_end - 1)); };
+    auto ask_pages = [&](int x) {
+        if (x < x_end) page = cache_page(c, b, t.seq, key_of(x));
+    };
+    u32x4 kr[NKB][KP], vr[VP];
+    float scale = 0.f, scale_v = 0.f;
+    auto ask_rows = [&](int x) {
+        if (x >= x_end) return;
+        held = __ballot(page >= 0);
+        row = cache_row(c, max(page, 0), head, key_of(x));
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+            // key of this lane's row of block kb: each group of lanes ends up with consecutive keys in its registers of S^T
+            const int j = (lq >> 2) * (4 * NKB) + kb * 4 + (lq & 3);
+            const uint8_t *src = c.k + (uint64_t)(uint32_t)__shfl((int)row, j) * T::ROW + g * PIECE;
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+                if constexpr (PIECE == 8) {
+                    const u32x2 h = *(const u32x2 *)src;
+                    kr[kb][i] = u32x4{h.x, h.y, 0, 0};
+                } else {
+                    kr[kb][i] = *(const u32x4 *)(src + i * 4 * PIECE);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            constexpr int PER_ROW = T::ROW / PIECE;
+            const int item = i * 64 + lane, j = item / PER_ROW, at = item % PER_ROW * PIECE;
+            const uint8_t *src = c.v + (uint64_t)(uint32_t)__shfl((int)row, j) * T::ROW + at;
+            if constexpr (PIECE == 8) {
+                const u32x2 h = *(const u32x2 *)src;
+                vr[i] = u32x4{h.x, h.y, 0, 0};
+            } else {
+                vr[i] = *(const u32x4 *)src;
+            }
+        }
+        if constexpr (BITS < 16) {
+            scale = c.k_scale[row];
+            scale_v = c.v_scale[row];
+        }
+    };
+
+    ask_pages(x0);
+
+    // queries as the B operand of S^T = K Q^T, features in the order of the keys' registers
+    u32x4 qf[NQ][D / 32];
+    int pos[NQ];
+    float back[NQ];   // what the scores of rows brought into binary16's range are multiplied by
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = t.row0 + min(n * 16 + lq, t.rows - 1), token = quotient(r, a.group, group_recip);
+        pos[n] = t.base + token;
+        back[n] = 1.f;
+        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + (head * a.group + r - token * a.group) * D + g * VALUES;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) qf[n][s] = *(const u32x4 *)(src + s * 8 / VALUES * 4 * VALUES + s * 8 % VALUES);
+        if constexpr (BITS < 16 && BF) {
+            const int shift = query_shift(four_max(largest_magnitude(qf[n])));
+            bring_into_binary16(qf[n], shift);
+            back[n] = two_to(shift);
+        }
+        if constexpr (BITS == 4)
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) qf[n][s] = in_nibble_order(qf[n][s]);
+    }
+
+    float4v o[NQ][D / 16];
+    float top[NQ], sum[NQ];   // (16 bits: top in units of the unscaled scores; sum: of this lane's keys)
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        top[n] = -INFINITY;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) o[n][e] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+
+    unsigned char *stage = lds + wave * T::STAGE;
+    float *sc = (float *)(stage + KT * VS);
+    ask_rows(x0);
+    ask_pages(x0 + x_stride);
+    for (; x0 < x_end; x0 += x_stride) {
+        const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
+        const uint64_t held_now = held;
+        const bool plain = x0 + KT <= x_end && held_now == ~(uint64_t)0 && key_last <= t.first_pos &&
+                           (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);   // every query sees every key
+        float4v s[NQ][NKB];
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) s[n][kb] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                u32x4 kf;
+                if constexpr (BITS == 16)
+                    kf = kr[kb][i];
+                else if constexpr (BITS == 8)
+                    kf = numbers_of_bytes(kr[kb][i / 2][(i & 1) * 2], kr[kb][i / 2][(i & 1) * 2 + 1]);
+                else
+                    kf = numbers_of_nibbles(kr[kb][0][i]);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[n][kb] = product<MBF>(kf, qf[n][i], s[n][kb]);
+            }
+        }
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            constexpr int PER_ROW = T::ROW / PIECE;
+            const int item = i * 64 + lane, j = item / PER_ROW, at = item % PER_ROW * PIECE;
+            if constexpr (PIECE == 8)
+                *(u32x2 *)(stage + j * VS + at) = u32x2{vr[i][0], vr[i][1]};
+            else
+                *(u32x4 *)(stage + j * VS + at) = vr[i];
+            if constexpr (BITS == 16)
+                if (!plain)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) odd |= odd_halves<BF>(vr[i][w]);
+        }
+        const bool some_odd = BITS == 16 && !plain && __any(odd != 0);
+        if constexpr (BITS < 16) {
+            if (lane < KT) {
+                const ValueScale v = value_scale(scale_v);
+                sc[lane] = scale * a.scale;
+                sc[KT + lane] = v.log;
+                sc[2 * KT + lane] = v.inverse;
+            }
+        }
+        wave_lds_fence();
+        ask_rows(x0 + x_stride);
+        ask_pages(x0 + 2 * x_stride);
+
+        uint32_t pk[NQ][NKB / 2][4];   // the weights, 16 bits, in the order of V^T's registers
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            if constexpr (BITS < 16) {
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb) {
+                    const int at = g * 4 * NKB + kb * 4;
+                    const float4v k4 = *(const float4v *)(sc + at), l4 = *(const float4v *)(sc + KT + at);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[n][kb][v] = fmaf(BF ? s[n][kb][v] * back[n] : s[n][kb][v], k4[v], l4[v]);
+                }
+            }
+            if (!plain) {
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int j = g * 4 * NKB + kb * 4 + v;
+                        const bool see = x0 + j < x_end && (held_now >> j & 1) && sees(pos[n], t.keys.key(x0 + j), a.window, a.sinks);
+                        s[n][kb][v] = see ? s[n][kb][v] : -INFINITY;
+                    }
+            }
+            float m = s[n][0][0];
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) m = fmaxf(m, s[n][kb][v]);
+            m = four_max(m);
+            // a query's results are shrunk only where its maximum has grown by more than 2^8: weights up to 256 are as exact as those up to 1
+            const float factor = BITS == 16 ? a.scale : 1.f;
+            const bool grown = (m - top[n]) * factor > 8.f || (top[n] == -INFINITY && m > -INFINITY);
+            if (__any(grown)) {
+                const float f = grown ? __builtin_amdgcn_exp2f((top[n] - m) * factor) : 1.f;
+                top[n] = grown ? m : top[n];
+                sum[n] *= f;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[n][e][v] *= f;
+            }
+            const float shift = top[n] == -INFINITY ? 0.f : -top[n] * factor;
+            float p[NKB][4];
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) p[kb][v] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(s[n][kb][v], factor, shift) : s[n][kb][v] + shift);
+                if constexpr (BITS == 16) {
+                    sum[n] += (p[kb][0] + p[kb][1]) + (p[kb][2] + p[kb][3]);
+                } else {
+                    const float4v i4 = *(const float4v *)(sc + 2 * KT + g * 4 * NKB + kb * 4);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) sum[n] = fmaf(p[kb][v], i4[v], sum[n]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < NKB / 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (BITS == 4)   // the order of numbers_of_nibbles
+                        pk[n][h][i] = cache_pair<false>(p[2 * h][i], p[2 * h + 1][i]);
+                    else
+                        pk[n][h][i] = cache_pair<MBF>(p[2 * h + (i >> 1)][(i & 1) * 2], p[2 * h + (i >> 1)][(i & 1) * 2 + 1]);
+                }
+            if (some_odd) {
+                for (int j = 0; j < KT; ++j) {
+                    const bool see = x0 + j < x_end && (held_now >> j & 1) && sees(pos[n], t.keys.key(x0 + j), a.window, a.sinks);
+#pragma unroll
+                    for (int e = 0; e < D / 16; ++e) {
+                        const u32x2 w = *(const u32x2 *)(stage + j * VS + (e * 16 + g * 4) * 2);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
+                            if (bad & 1) o[n][e][2 * i] += cache_number<BF>(pair & 0xFFFFu);
+                            if (bad >> 31) o[n][e][2 * i + 1] += cache_number<BF>(pair >> 16);
+                        }
+                    }
+                }
+            }
+        }
+        // O^T += V^T P^T
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {
+            if constexpr (BITS == 16) {
+                typedef __attribute__((address_space(3))) short4v *LdsShort4;
+                const unsigned char *src = stage + (g * 8 + (lq >> 2)) * VS + e * 32 + (lq & 3) * 8;
+                const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)src));
+                const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(src + 4 * VS)));
+                u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
+                if (some_odd) vf = without_odd<BF>(vf);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][e] = product<MBF>(vf, u32x4{pk[n][0][0], pk[n][0][1], pk[n][0][2], pk[n][0][3]}, o[n][e]);
+            } else {
+                typedef __attribute__((address_space(3))) int2v *LdsInt2;
+                const unsigned char *src = BITS == 8 ? stage + (g * 8 + (lq >> 1)) * VS + e * 16 + (lq & 1) * 8 : stage + (g * 16 + lq) * VS + e * 8;
+                int2v w;
+                if constexpr (BITS == 8)
+                    w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsInt2)src);
+                else
+                    w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((LdsInt2)src);
+                const uint32_t w0 = (uint32_t)w.x, w1 = (uint32_t)w.y;
+#pragma unroll
+                for (int h = 0; h < NKB / 2; ++h) {
+                    const u32x4 vf = BITS == 8 ? numbers_of_bytes(w0, w1) : numbers_of_nibbles(h ? w1 : w0);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][e] = product<false>(vf, u32x4{pk[n][h][0], pk[n][h][1], pk[n][h][2], pk[n][h][3]}, o[n][e]);
+                }
+            }
+        }
+        wave_lds_fence();
+    }
+
+    // join the waves: the upper half leaves its results in LDS, the lower half adds them, until one is left
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        sum[n] = four_sum(sum[n]);
+        if constexpr (BITS == 16) top[n] = top[n] == -INFINITY ? top[n] : top[n] * a.scale;
+    }
+    float *join = (float *)lds;
+#pragma unroll
+    for (int half = W / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float *to = join + ((wave - half) * ROWS + n * 16 + lq) * JS + g * 4;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) *(float4v *)(to + e * 16) = o[n][e];
+                if (g == 0) {
+                    tops[wave - half][n * 16 + lq] = top[n];
+                    weights[wave - half][n * 16 + lq] = sum[n];
+                }
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float theirs = tops[wave][n * 16 + lq], m = fmaxf(top[n], theirs);
+                const float f0 = top[n] == m ? 1.f : __builtin_amdgcn_exp2f(top[n] - m), f1 = theirs == m ? 1.f : __builtin_amdgcn_exp2f(theirs - m);
+                top[n] = m;
+                sum[n] = sum[n] * f0 + weights[wave][n * 16 + lq] * f1;
+                const float *from = join + (wave * ROWS + n * 16 + lq) * JS + g * 4;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) {
+                    const float4v x = *(const float4v *)(from + e * 16);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[n][e][v] = o[n][e][v] * f0 + x[v] * f1;
+                }
+            }
+        }
+    }
+    if (wave != 0) return;
+    const int64_t line = (int64_t)b.n_tokens * a.heads, plane = (int64_t)split * line;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        if (n * 16 + lq >= t.rows) continue;
+        const int r = t.row0 + n * 16 + lq, token = quotient(r, a.group, group_recip), q_head = head * a.group + r - token * a.group;
+        if (splits == 1) {
+            const float inv = sum[n] > 0.f ? 1.0f / sum[n] : (sum[n] == 0.f ? 0.f : sum[n]);
+            uint16_t *out = (uint16_t *)a.out + (t.first + token) * a.out_stride + q_head * D + g * 4;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e)
+                *(u32x2 *)(out + e * 16) = u32x2{cache_pair<BF>(o[n][e][0] * inv, o[n][e][1] * inv), cache_pair<BF>(o[n][e][2] * inv, o[n][e][3] * inv)};
+        } else {
+            const int64_t at = plane + (int64_t)(t.first + token) * a.heads + q_head;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) *(float4v *)(partials + at * D + g * 4 + e * 16) = o[n][e];
+            if (g == 0) {
+                float *ml = partials + (int64_t)splits * line * D + at * 2;
+                ml[0] = top[n];
+                ml[1] = sum[n];
+            }
+        }
+    }
+}
+
+template <int BITS, bool BF, int D>
+void launch_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
+    const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
+    auto go = [&](auto kernel, int waves) { launch(kernel, grid, dim3(64 * waves), 0, stream, a, gr, hr, sr, cut.splits, partials); };
+    if (cut.tile_rows == 16)
+        go(cache_few_kernel<BITS, BF, D, 1, 4>, 4);
+    else
+        go(cache_few_kernel<BITS, BF, D, 2, 4>, 4);
+}
+template <bool BF, int D>
+void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    if (a.bits == 16)
+        launch_few<16, BF, D>(a, cut, partials, stream);
+    else if (a.bits == 8)
+        launch_few<8, BF, D>(a, cut, partials, stream);
+    else
+        launch_few<4, BF, D>(a, cut, partials, stream);
+}
+
+}  // namespace
+
+hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+{
+    if (a.d == 64)
+        a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);
+    else
+        a.bf16 ? launch_bits<true, 128>(a, cut, partials, stream) : launch_bits<false, 128>(a, cut, partials, stream);
+    return hipGetLastError();
+}
+
+}  // namespace sti

@@ -1,28 +1,20 @@
-// Attention of many queries per sequence over a paged cache, on the matrix cores.
+// Attention of many queries per sequence, more than 32 on one key/value head, over a paged cache, on the matrix cores.
 //
 // Tiles of 32 WR queries of one key/value head; WK groups of WR waves walk the tile's keys KT at a time, each group its own steps.  Everything
 // is computed transposed, as in attention_core.hpp: S^T = K Q^T leaves a lane one query and 16 keys per 32, O^T = V^T P^T takes the weights in
-// the registers where they are, and the maximum of a query crosses only lanes l and l ^ 32.
-//
-//   t_j = c s_k[j] (q . code_k[j]) + log2 s_v[j],   P_j = 2^(t_j - m),   o = sum_j P_j code_v[j] / sum_j P_j / s_v[j]
-//
-// with codes (16 bits: s_k = s_v = 1): codes are exact in 16 bits, so that the only rounding in front of the matrix cores is that of the
-// weights, and a value's scale takes part in the maximum, so that a weight is largest where the value it carries is.  (The scale in the
-// value instead: another rounding per value; beside the weight without the maximum: weights of small values below 2^-14, the normal numbers of
-// binary16.)  Keys and values of a step go through registers to LDS (codes become 16-bit numbers on the way), one step ahead of the products;
-// V^T is read from its rows by the transposing LDS read.
-#include "cache_common.hpp"
+// the registers where they are, and the maximum of a query crosses only lanes l and l ^ 32.  The formula with scales is that of
+// cache_attention_few.hip.  Keys and values of a step go through registers to LDS (codes become binary16 on the way), one step ahead of the
+// products; V^T is read from its rows by the transposing LDS read.
+#include "cache_numbers.hpp"
 
 namespace sti {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef cache_u32x4 u32x4;
+typedef cache_u32x2 u32x2;
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
@@ -32,84 +24,10 @@ __device__ inline float16v product(u32x4 a, u32x4 b, float16v c)
     if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
-template <bool BF>
-__device__ inline float number(uint32_t half)
-{
-    if constexpr (BF) return __builtin_bit_cast(float, half << 16);
-    return (float)__builtin_bit_cast(_Float16, (uint16_t)half);
-}
-template <bool BF>
-__device__ inline uint32_t pair_bits(float lo, float hi)   // rounded to nearest even
-{
-    if constexpr (BF) {
-        const bf16x2 h = {(__bf16)lo, (__bf16)hi};
-        return __builtin_bit_cast(uint32_t, h);
-    }
-    return f16_pair_bits(lo, hi);
-}
-
-// Codes -> numbers of the matrix cores' type, exactly.  Binary16: a byte under 0x64 is 1024 + byte; bfloat16: through float32.
-__device__ inline uint32_t less(uint32_t pair, uint32_t by)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, pair) - __builtin_bit_cast(half2v, by));
-}
-template <bool BF>
-__device__ inline u32x4 numbers_of_bytes(uint32_t w0, uint32_t w1)   // 8 codes of 8 bits
-{
-    u32x4 out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w = i < 2 ? w0 : w1;
-        const int at = 16 * (i & 1);
-        if constexpr (BF) {
-            const float lo = (float)(int8_t)(w >> at), hi = (float)(int8_t)(w >> (at + 8));
-            out[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-        } else {
-            const uint32_t u = w ^ 0x80808080u;
-            out[i] = less(__builtin_amdgcn_perm(0x64646464u, u, i & 1 ? 0x04030402u : 0x04010400u), 0x64806480u);   // 1024 + 128
-        }
-    }
-    return out;
-}
-template <bool BF>
-__device__ inline u32x4 numbers_of_nibbles(uint32_t w)   // 8 codes of 4 bits
-{
-    const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
-    u32x4 out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (BF) {
-            const float lo = (float)((int)(even >> (8 * i) & 15) - 8), hi = (float)((int)(odd >> (8 * i) & 15) - 8);
-            out[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-        } else {
-            const uint32_t pair = __builtin_amdgcn_perm(odd, even, 0x0C040C00u + 0x00010001u * i) | 0x64006400u;
-            out[i] = less(pair, 0x64086408u);   // 1024 + 8
-        }
-    }
-    return out;
-}
-
-// Values that are not finite numbers (16 bits): 0 times one is not 0, so that in steps that not every query sees they are kept from the
-// matrix cores and added to the results of the queries that see them (a weight other than 1 would not change what comes of it).
-template <bool BF>
-__device__ inline uint32_t odd_halves(uint32_t pair)   // all bits of the halves whose exponent is the largest
-{
-    constexpr uint32_t kLow = BF ? 0x7F80u : 0x7C00u, kHigh = kLow << 16;
-    return ((pair & kLow) == kLow ? 0xFFFFu : 0u) | ((pair & kHigh) == kHigh ? 0xFFFF0000u : 0u);
-}
-template <bool BF>
-__device__ inline u32x4 without_odd(u32x4 v)
-{
-    u32x4 out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = v[i] & ~odd_halves<BF>(v[i]);
-    return out;
-}
-
 template <int BITS, int D, int WR, int WK>
 struct TileShape {
     static constexpr int KT = WR == 4 ? 64 : 32;         // keys of a step
-    static constexpr int BUFFERS = WR == 1 ? 1 : 2;      // a wave that has its step to itself writes behind its own reads
+    static constexpr int BUFFERS = 2;
     static constexpr int THREADS = 64 * WR;              // of a group
     static constexpr int KS = D + 8, VS = D + 32;        // halves per row in LDS: no two lanes of a read share a bank
     static constexpr int CHUNK = BITS == 16 ? 8 : 16;    // values of a request: 16 bytes, 8 of codes of 4 bits
@@ -123,11 +41,12 @@ struct TileShape {
 };
 
 template <int BITS, bool BF, int D, int WR, int WK>
-__global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, uint32_t group_recip, uint32_t tiles_recip, uint32_t splits_recip, int tiles,
-                                                             int splits, int pieces, int per_xcd, float *partials)
+__global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int tiles,
+                                                             int splits, float *partials)
 {
     using T = TileShape<BITS, D, WR, WK>;
     constexpr int KT = T::KT, KS = T::KS, VS = T::VS, ROWS = 32 * WR, NKB = KT / 32, ROW_BYTES = D * BITS / 8, CHUNK_BYTES = T::CHUNK * BITS / 8;
+    constexpr bool MBF = BITS == 16 && BF;   // the products' type
     __shared__ __attribute__((aligned(16))) unsigned char lds[T::LDS_BYTES];
     __shared__ float tops[WK][ROWS], weights[WK][ROWS];
     __shared__ int odd_step[WK][T::BUFFERS];   // the last step whose values, where some query may not see them, are not all finite
@@ -135,11 +54,10 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     const BatchView &b = a.batch;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const int g = lane >> 5, lr = lane & 31, tid = wr * 64 + lane;   // (tid: inside the group)
-    const int piece = piece_of_block(blockIdx.x, per_xcd);
-    if (piece >= pieces) return;
-    // (head, split, tile): the tiles of a head, which read the same keys, lie behind each other and go to one XCD
-    const int head_split = quotient(piece, tiles, tiles_recip), tile = piece - head_split * tiles;
-    const int head = quotient(head_split, splits, splits_recip), split = head_split - head * splits;
+    // blocks in the order (tile, split, head), the last tiles first: the heads of a tile, which share nothing, go to different XCDs and the tiles
+    // of a head, which read the same keys, to one or a few; the later a tile of a sequence, the more keys it has
+    const int tile_split = quotient(blockIdx.x, c.heads, heads_recip), head = blockIdx.x - tile_split * c.heads;
+    const int from_last = quotient(tile_split, splits, splits_recip), tile = tiles - 1 - from_last, split = tile_split - from_last * splits;
     const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
     if (t.seq < 0) return;
 
@@ -150,10 +68,19 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     const int wave_last = t.row0 + min(wr * 32 + 31, t.rows - 1);
     const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, group_recip), last_pos = t.base + quotient(wave_last, a.group, group_recip);
     u32x4 qf[D / 16];
+    float back = 1.f;   // what the scores of a row brought into binary16's range are multiplied by
     {
         const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + s * 16);
+        if constexpr (BITS < 16 && BF) {
+            const int shift = query_shift(pair_max(across_32(largest_magnitude(qf))));
+            bring_into_binary16(qf, shift);
+            back = two_to(shift);
+        }
+        if constexpr (BITS == 4)
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) qf[s] = in_nibble_order(qf[s]);
     }
 
     const int steps = (t.keys.count + KT - 1) / KT, share = (steps + splits - 1) / splits;
@@ -180,11 +107,11 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     };
     auto ask_rows = [&](int x0) {
         if (x0 >= x_end) return;
+        const uint32_t of_key = cache_row(c, max(pages, 0), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));   // row of key `lane` % KT
 #pragma unroll
         for (int i = 0; i < T::ITEMS; ++i) {
             const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, part = item % T::ROW_CHUNKS;
-            const int page = max(__shfl(pages, r), 0);
-            const int64_t at = cache_row(c, page, head, t.keys.key(min(x0 + r, x_end - 1))) * ROW_BYTES + part * CHUNK_BYTES;
+            const uint64_t at = (uint64_t)(uint32_t)__shfl((int)of_key, r) * ROW_BYTES + part * CHUNK_BYTES;
             if constexpr (BITS == 4) {
                 const u32x2 k2 = *(const u32x2 *)(c.k + at), v2 = *(const u32x2 *)(c.v + at);
                 kr[i] = u32x4{k2.x, k2.y, 0, 0};
@@ -195,9 +122,8 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             }
         }
         if constexpr (BITS < 16) {
-            const int64_t at = cache_row(c, max(pages, 0), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));
-            scale_k = c.k_scale[at];
-            scale_v = c.v_scale[at];
+            scale_k = c.k_scale[of_key];
+            scale_v = c.v_scale[of_key];
         }
     };
     auto step_lds = [&](int buffer) { return lds + (wk * T::BUFFERS + buffer) * T::STEP_BYTES; };
@@ -224,46 +150,38 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                 kd[0] = kr[i];
                 vd[0] = vr[i];
             } else if constexpr (BITS == 8) {
-                kd[0] = numbers_of_bytes<BF>(kr[i][0], kr[i][1]);
-                kd[1] = numbers_of_bytes<BF>(kr[i][2], kr[i][3]);
-                vd[0] = numbers_of_bytes<BF>(vr[i][0], vr[i][1]);
-                vd[1] = numbers_of_bytes<BF>(vr[i][2], vr[i][3]);
+                kd[0] = numbers_of_bytes(kr[i][0], kr[i][1]);
+                kd[1] = numbers_of_bytes(kr[i][2], kr[i][3]);
+                vd[0] = numbers_of_bytes(vr[i][0], vr[i][1]);
+                vd[1] = numbers_of_bytes(vr[i][2], vr[i][3]);
             } else {
-                kd[0] = numbers_of_nibbles<BF>(kr[i][0]);
-                kd[1] = numbers_of_nibbles<BF>(kr[i][1]);
-                vd[0] = numbers_of_nibbles<BF>(vr[i][0]);
-                vd[1] = numbers_of_nibbles<BF>(vr[i][1]);
+                kd[0] = numbers_of_nibbles(kr[i][0]);
+                kd[1] = numbers_of_nibbles(kr[i][1]);
+                vd[0] = numbers_of_nibbles(vr[i][0]);
+                vd[1] = numbers_of_nibbles(vr[i][1]);
             }
         }
         if constexpr (BITS < 16) {
             float *sc = (float *)(vs + KT * VS);
             if (tid < KT) {
-                // a row of zeros has scale 0: any small one serves, its weight counts in the sum alone
-                const float s = scale_v == 0.f ? 0x1p-100f : scale_v;
+                const ValueScale s = value_scale(scale_v);
                 sc[tid] = scale_k * a.scale;
-                sc[KT + tid] = __builtin_amdgcn_logf(s);   // log2
-                sc[2 * KT + tid] = 1.0f / s;
+                sc[KT + tid] = s.log;
+                sc[2 * KT + tid] = s.inverse;
             }
         }
     };
-    auto meet = [&]() {
-        if constexpr (WR == 1)
-            wave_lds_fence();
-        else
-            __syncthreads();
-    };
-
     if (lane == 0)
         for (int i = 0; i < T::BUFFERS; ++i) odd_step[wk][i] = -1;   // (the waves of a group write the same; a find comes behind the barrier)
-    meet();
+    __syncthreads();
     ask_pages(x_first);
     ask_rows(x_first);
     pages_now = pages;
     ask_pages(x_first + x_stride);
     put_rows(0, 0, pages_now);
-    meet();
+    __syncthreads();
     for (int n = 0; n < rounds; ++n) {
-        const int x0 = x_first + n * x_stride, buffer = T::BUFFERS == 2 ? n & 1 : 0;
+        const int x0 = x_first + n * x_stride, buffer = n & 1;
         ask_rows(x0 + x_stride);
         const int pages_next = pages;
         ask_pages(x0 + 2 * x_stride);
@@ -282,9 +200,8 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                 for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
-                    s[kb] = product<BF>(*(const u32x4 *)(ks + (kb * 32 + lr) * KS + i * 16 + g * 8), qf[i], s[kb]);
+                    s[kb] = product<MBF>(*(const u32x4 *)(ks + (kb * 32 + lr) * KS + i * 16 + g * 8), qf[i], s[kb]);
             }
-            uint32_t seen[NKB];   // bit v: this lane's query sees the key of register v
             if constexpr (BITS < 16) {
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb)
@@ -292,18 +209,16 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                     for (int v4 = 0; v4 < 4; ++v4) {
                         const float4v k4 = *(const float4v *)(sc + kb * 32 + v4 * 8 + g * 4), l4 = *(const float4v *)(sc + KT + kb * 32 + v4 * 8 + g * 4);
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) s[kb][v4 * 4 + v] = fmaf(s[kb][v4 * 4 + v], k4[v], l4[v]);
+                        for (int v = 0; v < 4; ++v) s[kb][v4 * 4 + v] = fmaf(BF ? s[kb][v4 * 4 + v] * back : s[kb][v4 * 4 + v], k4[v], l4[v]);
                     }
             }
             if (!plain) {
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb) {
-                    seen[kb] = 0;
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const int j = kb * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
                         const bool see = x0 + j < x_end && (held >> j & 1) && sees(pos, t.keys.key(x0 + j), a.window, a.sinks);
-                        seen[kb] |= see ? 1u << v : 0u;
                         s[kb][v] = see ? s[kb][v] : -INFINITY;
                     }
                 }
@@ -338,8 +253,8 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
                                 const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
-                                if (bad & 1) o[e][v4 * 4 + 2 * i] += number<BF>(pair & 0xFFFFu);
-                                if (bad >> 31) o[e][v4 * 4 + 2 * i + 1] += number<BF>(pair >> 16);
+                                if (bad & 1) o[e][v4 * 4 + 2 * i] += cache_number<BF>(pair & 0xFFFFu);
+                                if (bad >> 31) o[e][v4 * 4 + 2 * i + 1] += cache_number<BF>(pair >> 16);
                             }
                         }
                 }
@@ -358,13 +273,10 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                     } else {
                         const float4v i4 = *(const float4v *)(sc + 2 * KT + kb * 32 + v4 * 8 + g * 4);
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const float w = fmaf(p[v], i4[v], sum);
-                            sum = plain || (seen[kb] >> (v4 * 4 + v) & 1) ? w : sum;   // (a scale that is not seen may be NaN)
-                        }
+                        for (int v = 0; v < 4; ++v) sum = fmaf(p[v], i4[v], sum);
                     }
-                    pk[v4 * 2] = pair_bits<BF>(p[0], p[1]);
-                    pk[v4 * 2 + 1] = pair_bits<BF>(p[2], p[3]);
+                    pk[v4 * 2] = cache_pair<MBF>(p[0], p[1]);
+                    pk[v4 * 2 + 1] = cache_pair<MBF>(p[2], p[3]);
                 }
                 // O^T += V^T P^T, 16 keys at a time in the order of the registers
 #pragma unroll
@@ -378,17 +290,32 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + 8 * VS + e * 32)));
                         u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
                         if (BITS == 16 && odd) vf = without_odd<BF>(vf);
-                        o[e] = product<BF>(vf, pf, o[e]);
+                        o[e] = product<MBF>(vf, pf, o[e]);
                     }
                 }
             }
         }
-        if constexpr (T::BUFFERS == 1) meet();
-        put_rows(T::BUFFERS == 2 ? (n + 1) & 1 : 0, n + 1, pages_next);
-        meet();
+        put_rows((n + 1) & 1, n + 1, pages_next);
+        __syncthreads();
         pages_now = pages_next;
     }
 
+    if constexpr (BITS == 4) {
+        // features 0 4 1 5 and 2 6 3 7 of each eight (numbers_of_nibbles) to 0 1 2 3 and 4 5 6 7
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) {
+                const float x0 = o[e][v], x1 = o[e][v + 1], x2 = o[e][v + 2], x3 = o[e][v + 3];
+                const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1), false, false);
+                const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x2), __builtin_bit_cast(uint32_t, x3), false, false);
+                const uint32_t y0 = a[0], y2 = a[1], y1 = b[0], y3 = b[1];
+                o[e][v] = __builtin_bit_cast(float, y0);
+                o[e][v + 1] = __builtin_bit_cast(float, y1);
+                o[e][v + 2] = __builtin_bit_cast(float, y2);
+                o[e][v + 3] = __builtin_bit_cast(float, y3);
+            }
+    }
     sum = pair_sum(across_32(sum));
     if constexpr (BITS == 16) top = top == -INFINITY ? top : top * a.scale;
     const int64_t line = (int64_t)b.n_tokens * a.heads, plane = (int64_t)split * line;
@@ -402,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             for (int e = 0; e < D / 32; ++e)
 #pragma unroll
                 for (int v4 = 0; v4 < 4; ++v4) {
-                    const u32x2 w = {pair_bits<BF>(o[e][v4 * 4] * inv, o[e][v4 * 4 + 1] * inv), pair_bits<BF>(o[e][v4 * 4 + 2] * inv, o[e][v4 * 4 + 3] * inv)};
+                    const u32x2 w = {cache_pair<BF>(o[e][v4 * 4] * inv, o[e][v4 * 4 + 1] * inv), cache_pair<BF>(o[e][v4 * 4 + 2] * inv, o[e][v4 * 4 + 3] * inv)};
                     *(u32x2 *)(out + e * 32 + v4 * 8) = w;
                 }
         } else {
@@ -450,7 +377,7 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             const int rr = t.row0 + r, tok = quotient(rr, a.group, group_recip), qh = head * a.group + rr - tok * a.group;
             if (splits == 1) {
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-                const u32x2 w = {pair_bits<BF>(v[0] * inv, v[1] * inv), pair_bits<BF>(v[2] * inv, v[3] * inv)};
+                const u32x2 w = {cache_pair<BF>(v[0] * inv, v[1] * inv), cache_pair<BF>(v[2] * inv, v[3] * inv)};
                 *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + at) = w;
             } else {
                 const int64_t to = plane + (int64_t)(t.first + tok) * a.heads + qh;
@@ -468,13 +395,10 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
 template <int BITS, bool BF, int D>
 void launch_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
 {
-    const int pieces = (int)(cut.tiles * cut.splits * a.cache.heads), per_xcd = pieces_per_xcd(pieces);
-    const dim3 grid((uint32_t)(per_xcd * 8));
-    const uint32_t gr = reciprocal((uint32_t)a.group), tr = reciprocal((uint32_t)cut.tiles), sr = reciprocal((uint32_t)cut.splits);
-    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, tr, sr, (int)cut.tiles, cut.splits, pieces, per_xcd, partials); };
-    if (cut.tile_rows == 32)
-        go(cache_tiles_kernel<BITS, BF, D, 1, 4>);
-    else if (cut.tile_rows == 64)
+    const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
+    const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, hr, sr, (int)cut.tiles, cut.splits, partials); };
+    if (cut.tile_rows == 64)
         go(cache_tiles_kernel<BITS, BF, D, 2, 2>);
     else
         go(cache_tiles_kernel<BITS, BF, D, 4, 1>);

@@ -21,10 +21,10 @@ struct BatchView {
     int32_t n_seqs, n_tokens, max_pages;
 };
 
-// The row of (page, head, slot); beyond 2^31 rows in a large pool, and beyond 2^32 bytes in an ordinary one.
-__device__ inline int64_t cache_row(const CacheView &c, int page, int head, int position)
+// The row of (page, head, slot): below 2^32 (the entry points' limit), while its bytes may lie beyond 2^32 in an ordinary pool.
+__device__ inline uint32_t cache_row(const CacheView &c, int page, int head, int position)
 {
-    return (((int64_t)page * c.heads + head) << c.page_shift) + (position & ((1 << c.page_shift) - 1));
+    return (((uint32_t)page * c.heads + head) << c.page_shift) + (position & ((1 << c.page_shift) - 1));
 }
 // Page of a position (0 <= position < capacity), or -1 where the table names none of the pool's.
 __device__ inline int cache_page(const CacheView &c, const BatchView &b, int seq, int position)
@@ -146,7 +146,8 @@ inline size_t partial_bytes(int64_t n_tokens, int heads, int d, int splits)
     return splits > 1 ? (size_t)splits * n_tokens * heads * (d + 2) * sizeof(float) : 0;
 }
 hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);
-hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);   // tile_rows 32 and more
+hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);     // tile_rows 16 and 32
+hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);   // 64 and 128
 hipError_t launch_cache_join(const AttentionCall &a, int splits, const float *partials, hipStream_t stream);
 
 }  // namespace sti

@@ -1,0 +1,143 @@
+// Codes of the cache as operands of the matrix cores, exactly: a byte or nibble in the low bits of binary16 1024 makes 1024 + code, from
+// which the constant is taken.  Caches of 8 and 4 bits multiply in binary16 whatever the type of the queries: codes and weights (at most
+// 2^8, none below 2^-24 that matters) have room there and keep 11 bits; rows of bfloat16 queries are brought into its range by a
+// power of two (query_shift).
+#pragma once
+#include "cache_common.hpp"
+
+namespace sti {
+
+typedef uint32_t cache_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t cache_u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ inline uint32_t pair_minus(uint32_t pair, uint32_t constant)
+{
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, pair) - __builtin_bit_cast(half2v, constant));
+}
+__device__ inline uint32_t pair_scaled(uint32_t pair, uint32_t factor, uint32_t addend)
+{
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    const half2v r = __builtin_elementwise_fma(__builtin_bit_cast(half2v, pair), __builtin_bit_cast(half2v, factor), __builtin_bit_cast(half2v, addend));
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// 8 codes of 8 bits, in order: 1.25 instructions each
+__device__ inline cache_u32x4 numbers_of_bytes(uint32_t w0, uint32_t w1)
+{
+    cache_u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = (i < 2 ? w0 : w1) ^ 0x80808080u;   // code + 128
+        out[i] = pair_minus(__builtin_amdgcn_perm(0x64646464u, u, i & 1 ? 0x04030402u : 0x04010400u), 0x64806480u);   // 1024 + 128
+    }
+    return out;
+}
+// 8 codes of 4 bits in the order 0 4 1 5 2 6 3 7: 1.1 instructions each
+__device__ inline cache_u32x4 numbers_of_nibbles(uint32_t w)
+{
+    cache_u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t v = i ? w >> 8 : w;
+        out[2 * i] = pair_minus((v & 0x000F000Fu) | 0x64006400u, 0x64086408u);                        // 1024 + 8
+        out[2 * i + 1] = pair_scaled((v & 0x00F000F0u) | 0x64006400u, 0x2C002C00u, 0xD480D480u);     // (1024 + 16 code) / 16 - (64 + 8)
+    }
+    return out;
+}
+// the same order for 8 values of 16 bits
+__device__ inline cache_u32x4 in_nibble_order(cache_u32x4 v)
+{
+    const uint32_t a = v[0], b = v[1], c = v[2], d = v[3];
+    return cache_u32x4{__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u),
+                       __builtin_amdgcn_perm(d, b, 0x05040100u), __builtin_amdgcn_perm(d, b, 0x07060302u)};
+}
+
+// Values that are not finite numbers (caches of 16 bits): 0 times one is not 0, so that in steps that not every query sees they are kept from
+// the matrix cores and added to the results of the queries that see them (a weight other than 1 would not change what comes of it).
+template <bool BF>
+__device__ inline uint32_t odd_halves(uint32_t pair)   // all bits of the halves whose exponent is the largest
+{
+    constexpr uint32_t kLow = BF ? 0x7F80u : 0x7C00u, kHigh = kLow << 16;
+    return ((pair & kLow) == kLow ? 0xFFFFu : 0u) | ((pair & kHigh) == kHigh ? 0xFFFF0000u : 0u);
+}
+template <bool BF>
+__device__ inline cache_u32x4 without_odd(cache_u32x4 v)
+{
+    cache_u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t p = v[i];
+        out[i] = p & ~odd_halves<BF>(p);
+    }
+    return out;
+}
+template <bool BF>
+__device__ inline float cache_number(uint32_t half)
+{
+    if constexpr (BF) return __builtin_bit_cast(float, half << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)half);
+}
+template <bool BF>
+__device__ inline uint32_t cache_pair(float lo, float hi)   // rounded to nearest even
+{
+    if constexpr (BF) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const bf16x2 h = {(__bf16)lo, (__bf16)hi};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+    return f16_pair_bits(lo, hi);
+}
+
+// A value's scale beside its weight.  A row of zeros has scale 0: any small one serves, its weight counts in the sum alone.  A scale that is NaN
+// makes the weight NaN where it is seen; where it is not, the weight is 0, and what it is multiplied by has to be finite.
+struct ValueScale {
+    float log, inverse;
+};
+__device__ inline ValueScale value_scale(float scale)
+{
+    const float s = scale < 0x1p-100f ? 0x1p-100f : scale;
+    return {__builtin_amdgcn_logf(s), s == s ? __builtin_amdgcn_rcpf(s) : 1.f};   // (base 2; the reciprocal to one unit in the last place)
+}
+
+// Power of two 2^-shift that brings a bfloat16 row with this largest magnitude to 2^14 .. 2^15 (rows of zeros, of
+// subnormal numbers and rows that are not finite stay near where they are): what is lost, values below 2^-39 of the largest, is beyond
+// float32's own sums.
+__device__ inline int query_shift(float most)
+{
+    const int exponent = (int)(__builtin_bit_cast(uint32_t, most) >> 23 & 0xFF);
+    return exponent == 0 || exponent == 0xFF ? 0 : max(exponent - 127 - 14, -125);   // (2^-shift and 2^shift are normal numbers)
+}
+__device__ inline float two_to(int e)   // -126 .. 127
+{
+    return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+}
+
+// A lane's pieces of a bfloat16 row (COUNT of 8 values) -> binary16 in place, times 2^-shift.
+template <int COUNT>
+__device__ inline void bring_into_binary16(cache_u32x4 (&q)[COUNT], int shift)
+{
+    const float into = two_to(-shift);
+#pragma unroll
+    for (int s = 0; s < COUNT; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = q[s][i];
+            q[s][i] = f16_pair_bits(cache_number<true>(p & 0xFFFFu) * into, cache_number<true>(p >> 16) * into);
+        }
+}
+template <int COUNT>
+__device__ inline float largest_magnitude(const cache_u32x4 (&q)[COUNT])   // of bfloat16 values, a NaN's bits as they compare
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int s = 0; s < COUNT; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = q[s][i] & 0x7FFF7FFFu;
+            most = max(most, max(p & 0xFFFFu, p >> 16));
+        }
+    return __builtin_bit_cast(float, most << 16);
+}
+
+}  // namespace sti
