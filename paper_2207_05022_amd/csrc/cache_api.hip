@@ -168,9 +168,10 @@ sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *ba
     a.out = out;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    st = timed_call(STI_K_ATTENTION, [&] { return launch_cache_attention(a, cut, (float *)workspace, (hipStream_t)hip_stream); });
+    const Partials partials = partials_at(workspace, batch->n_tokens, n_heads, cache->d_head, cut.splits);
+    st = timed_call(STI_K_ATTENTION, [&] { return launch_cache_attention(a, cut, partials, (hipStream_t)hip_stream); });
     if (st != STI_OK || cut.splits == 1) return st;
-    return timed_call(STI_K_ATTENTION, [&] { return launch_cache_join(a, cut.splits, (const float *)workspace, (hipStream_t)hip_stream); });
+    return timed_call(STI_K_ATTENTION, [&] { return launch_cache_join(a, cut.splits, partials, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Attention of up to 32 queries that share keys over a paged cache, on the matrix cores: single tokens, drafts of a few, groups of heads
+// Attention of up to 16 queries that share keys over a paged cache, on the matrix cores: single tokens, drafts of a few, groups of heads
 // on one key/value head.
 //
 //   t_j = c s_k[j] (q . code_k[j]) + log2 s_v[j],   P_j = 2^(t_j - m),   o = sum_j P_j code_v[j] / sum_j P_j / s_v[j]
@@ -32,7 +32,7 @@ __device__ inline float4v product(u32x4 a, u32x4 b, float4v c)
 __device__ inline float four_max(float v) { return pair_max(across_32(pair_max(across_16(v)))); }
 __device__ inline float four_sum(float v) { return pair_sum(across_32(pair_sum(across_16(v)))); }
 
-template <int BITS, int D, int NQ, int W>
+template <int BITS, int D, int W>
 struct FewShape {
     static constexpr int KT = BITS == 4 ? 64 : 32, NKB = KT / 16;        // keys of a step, blocks of 16 of them
     static constexpr int ROW = D * BITS / 8;                              // bytes of a row
@@ -43,17 +43,17 @@ struct FewShape {
     static constexpr int VS = ROW + 16;                                   // bytes per row in LDS: no two lanes of a read share a bank
     static constexpr int STAGE = KT * VS + (BITS < 16 ? 3 * KT * 4 : 0);
     static constexpr int JS = D + 4, HALF = W > 1 ? W / 2 : 1;
-    static constexpr int JOIN = HALF * 16 * NQ * JS * 4;
+    static constexpr int JOIN = HALF * 16 * JS * 4;
     static constexpr int LDS = W * STAGE > JOIN ? W * STAGE : JOIN;
 };
 
-// ROWS = 16 NQ queries of one key/value head, W waves
-template <int BITS, bool BF, int D, int NQ, int W>
+// 16 queries of one key/value head, W waves
+template <int BITS, bool BF, int D, int W>
 __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int splits,
-                                                              float *partials)
+                                                              int per_split, Partials partials)
 {
-    using T = FewShape<BITS, D, NQ, W>;
-    constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16 * NQ, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
+    using T = FewShape<BITS, D, W>;
+    constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16, NQ = 1, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
     constexpr bool MBF = BITS == 16 && BF;   // the products' type
     __shared__ __attribute__((aligned(16))) unsigned char lds[T::LDS];
     __shared__ float tops[T::HALF][ROWS], weights[T::HALF][ROWS];
@@ -66,9 +66,10 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
     const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
     if (t.seq < 0) return;
 
-    const int steps = (t.keys.count + KT - 1) / KT, share = (steps + splits - 1) / splits;
-    const int x_end = min(t.keys.count, (split + 1) * share * KT), x_stride = W * KT;
-    int x0 = (split * share + wave) * KT;
+    const KeyShare share = key_share(t.keys, split, per_split);
+    if (split >= share.parts) return;
+    const int x_end = share.end, x_stride = W * KT;
+    int x0 = share.begin + wave * KT;
 
     // row of key `lane` % KT of a step in the pool, and whether its page is there
     int page = -1;
@@ -155,11 +156,16 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
     float *sc = (float *)(stage + KT * VS);
     ask_rows(x0);
     ask_pages(x0 + x_stride);
-    for (; x0 < x_end; x0 += x_stride) {
-        const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
-        const uint64_t held_now = held;
-        const bool plain = x0 + KT <= x_end && held_now == ~(uint64_t)0 && key_last <= t.first_pos &&
-                           (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);   // every query sees every key
+    uint64_t held_now = 0;
+    // whether every query sees every key of the step at x0
+    auto seen_by_all = [&]() {
+        const int key_first = t.keys.key(x0), key_last = t.keys.key(x0 + KT - 1);
+        return x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= t.first_pos &&
+               (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);
+    };
+    auto compute = [&](auto all_see) {
+        constexpr bool PLAIN = decltype(all_see)::value;
+        held_now = held;
         float4v s[NQ][NKB];
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
@@ -187,12 +193,11 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                 *(u32x2 *)(stage + j * VS + at) = u32x2{vr[i][0], vr[i][1]};
             else
                 *(u32x4 *)(stage + j * VS + at) = vr[i];
-            if constexpr (BITS == 16)
-                if (!plain)
+            if constexpr (BITS == 16 && !PLAIN)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) odd |= odd_halves<BF>(vr[i][w]);
         }
-        const bool some_odd = BITS == 16 && !plain && __any(odd != 0);
+        const bool some_odd = BITS == 16 && !PLAIN && __any(odd != 0);
         if constexpr (BITS < 16) {
             if (lane < KT) {
                 const ValueScale v = value_scale(scale_v);
@@ -217,15 +222,14 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                     for (int v = 0; v < 4; ++v) s[n][kb][v] = fmaf(BF ? s[n][kb][v] * back[n] : s[n][kb][v], k4[v], l4[v]);
                 }
             }
-            if (!plain) {
+            uint64_t seen = 0;
+            if constexpr (!PLAIN) {
+                seen = seen_keys(t.keys, pos[n], a.window, a.sinks, x0, x_end) & held_now;
+                const uint32_t mine = (uint32_t)(seen >> (g * 4 * NKB));
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const int j = g * 4 * NKB + kb * 4 + v;
-                        const bool see = x0 + j < x_end && (held_now >> j & 1) && sees(pos[n], t.keys.key(x0 + j), a.window, a.sinks);
-                        s[n][kb][v] = see ? s[n][kb][v] : -INFINITY;
-                    }
+                    for (int v = 0; v < 4; ++v) s[n][kb][v] = mine & (1u << (kb * 4 + v)) ? s[n][kb][v] : -INFINITY;
             }
             float m = s[n][0][0];
 #pragma unroll
@@ -269,8 +273,9 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                         pk[n][h][i] = cache_pair<MBF>(p[2 * h + (i >> 1)][(i & 1) * 2], p[2 * h + (i >> 1)][(i & 1) * 2 + 1]);
                 }
             if (some_odd) {
+#pragma unroll 1
                 for (int j = 0; j < KT; ++j) {
-                    const bool see = x0 + j < x_end && (held_now >> j & 1) && sees(pos[n], t.keys.key(x0 + j), a.window, a.sinks);
+                    const bool see = seen >> j & 1;
 #pragma unroll
                     for (int e = 0; e < D / 16; ++e) {
                         const u32x2 w = *(const u32x2 *)(stage + j * VS + (e * 16 + g * 4) * 2);
@@ -293,7 +298,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                 const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)src));
                 const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(src + 4 * VS)));
                 u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
-                if (some_odd) vf = without_odd<BF>(vf);
+                if (!PLAIN && some_odd) vf = without_odd<BF>(vf);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) o[n][e] = product<MBF>(vf, u32x4{pk[n][0][0], pk[n][0][1], pk[n][0][2], pk[n][0][3]}, o[n][e]);
             } else {
@@ -314,6 +319,17 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
             }
         }
         wave_lds_fence();
+    };
+    // (loops of their own: what two paths leave in registers would be copied where they meet)
+    while (x0 < x_end) {
+        while (x0 < x_end && seen_by_all()) {
+            compute(std::true_type());
+            x0 += x_stride;
+        }
+        if (x0 < x_end) {
+            compute(std::false_type());
+            x0 += x_stride;
+        }
     }
 
     // join the waves: the upper half leaves its results in LDS, the lower half adds them, until one is left
@@ -357,43 +373,38 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
         }
     }
     if (wave != 0) return;
-    const int64_t line = (int64_t)b.n_tokens * a.heads, plane = (int64_t)split * line;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         if (n * 16 + lq >= t.rows) continue;
         const int r = t.row0 + n * 16 + lq, token = quotient(r, a.group, group_recip), q_head = head * a.group + r - token * a.group;
-        if (splits == 1) {
+        const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, plane = (int64_t)split * b.n_tokens * a.heads + to_row;
+        if (share.parts == 1) {
             const float inv = sum[n] > 0.f ? 1.0f / sum[n] : (sum[n] == 0.f ? 0.f : sum[n]);
             uint16_t *out = (uint16_t *)a.out + (t.first + token) * a.out_stride + q_head * D + g * 4;
 #pragma unroll
             for (int e = 0; e < D / 16; ++e)
                 *(u32x2 *)(out + e * 16) = u32x2{cache_pair<BF>(o[n][e][0] * inv, o[n][e][1] * inv), cache_pair<BF>(o[n][e][2] * inv, o[n][e][3] * inv)};
         } else {
-            const int64_t at = plane + (int64_t)(t.first + token) * a.heads + q_head;
 #pragma unroll
-            for (int e = 0; e < D / 16; ++e) *(float4v *)(partials + at * D + g * 4 + e * 16) = o[n][e];
-            if (g == 0) {
-                float *ml = partials + (int64_t)splits * line * D + at * 2;
-                ml[0] = top[n];
-                ml[1] = sum[n];
-            }
+            for (int e = 0; e < D / 16; ++e) *(float4v *)(partials.sums + plane * D + g * 4 + e * 16) = o[n][e];
+        }
+        if (splits > 1 && g == 0) {
+            partials.top_weight[plane * 2] = top[n];
+            partials.top_weight[plane * 2 + 1] = sum[n];
+            if (split == 0) partials.parts[to_row] = share.parts;
         }
     }
 }
 
 template <int BITS, bool BF, int D>
-void launch_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+void launch_few(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
     const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    auto go = [&](auto kernel, int waves) { launch(kernel, grid, dim3(64 * waves), 0, stream, a, gr, hr, sr, cut.splits, partials); };
-    if (cut.tile_rows == 16)
-        go(cache_few_kernel<BITS, BF, D, 1, 4>, 4);
-    else
-        go(cache_few_kernel<BITS, BF, D, 2, 4>, 4);
+    launch(cache_few_kernel<BITS, BF, D, 4>, grid, dim3(256), 0, stream, a, gr, hr, sr, cut.splits, cut.keys, partials);
 }
 template <bool BF, int D>
-void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+void launch_bits(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     if (a.bits == 16)
         launch_few<16, BF, D>(a, cut, partials, stream);
@@ -405,7 +416,7 @@ void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partial
 
 }  // namespace
 
-hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     if (a.d == 64)
         a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);

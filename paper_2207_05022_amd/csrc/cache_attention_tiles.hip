@@ -1,4 +1,4 @@
-// Attention of many queries per sequence, more than 32 on one key/value head, over a paged cache, on the matrix cores.
+// Attention of many queries per sequence, more than 16 on one key/value head, over a paged cache, on the matrix cores.
 //
 // Tiles of 32 WR queries of one key/value head; WK groups of WR waves walk the tile's keys KT at a time, each group its own steps.  Everything
 // is computed transposed, as in attention_core.hpp: S^T = K Q^T leaves a lane one query and 16 keys per 32, O^T = V^T P^T takes the weights in
@@ -42,7 +42,7 @@ struct TileShape {
 
 template <int BITS, bool BF, int D, int WR, int WK>
 __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int tiles,
-                                                             int splits, float *partials)
+                                                             int splits, int per_split, Partials partials)
 {
     using T = TileShape<BITS, D, WR, WK>;
     constexpr int KT = T::KT, KS = T::KS, VS = T::VS, ROWS = 32 * WR, NKB = KT / 32, ROW_BYTES = D * BITS / 8, CHUNK_BYTES = T::CHUNK * BITS / 8;
@@ -60,6 +60,8 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     const int from_last = quotient(tile_split, splits, splits_recip), tile = tiles - 1 - from_last, split = tile_split - from_last * splits;
     const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
     if (t.seq < 0) return;
+    const KeyShare share = key_share(t.keys, split, per_split);
+    if (split >= share.parts) return;
 
     // this lane's query as the B operand of S^T = K Q^T
     const int row = t.row0 + min(wr * 32 + lr, t.rows - 1), token = quotient(row, a.group, group_recip);
@@ -83,12 +85,9 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             for (int s = 0; s < D / 16; ++s) qf[s] = in_nibble_order(qf[s]);
     }
 
-    const int steps = (t.keys.count + KT - 1) / KT, share = (steps + splits - 1) / splits;
-    const int step0 = split * share, step1 = min(steps, step0 + share);
-    const int x_end = min(t.keys.count, step1 * KT);
-    const int rounds = max(0, (step1 - step0 + WK - 1) / WK);   // the same for all groups: they meet at barriers
-
-    const int x_first = (step0 + wk) * KT, x_stride = WK * KT;   // the group's steps
+    const int x_end = share.end, steps = (x_end - share.begin + KT - 1) / KT;
+    const int rounds = (steps + WK - 1) / WK;   // the same for all groups: they meet at barriers
+    const int x_first = share.begin + wk * KT, x_stride = WK * KT;   // the group's steps
 
     float16v o[D / 32];
 #pragma unroll
@@ -187,12 +186,10 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
         ask_pages(x0 + 2 * x_stride);
         const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
         const bool none = idle || x0 >= x_end || key_first > last_pos || (a.window > 0 && key_first >= a.sinks && key_last <= first_pos - a.window);
-        if (!none) {
+        auto compute = [&](auto all_see, uint64_t held) {   // all_see: whether every query of the wave sees every key of the step
+            constexpr bool PLAIN = decltype(all_see)::value;
             const uint16_t *ks = (const uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
             const float *sc = (const float *)(vs + KT * VS);
-            const uint64_t held = __ballot(pages_now >= 0);   // bit j: the page of key j is there (KT 32: bits twice)
-            const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
-                               (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);
             float16v s[NKB];
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb) {
@@ -212,15 +209,14 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                         for (int v = 0; v < 4; ++v) s[kb][v4 * 4 + v] = fmaf(BF ? s[kb][v4 * 4 + v] * back : s[kb][v4 * 4 + v], k4[v], l4[v]);
                     }
             }
-            if (!plain) {
+            uint64_t seen = 0;
+            if constexpr (!PLAIN) {
+                seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held;
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb) {
+                    const uint32_t mine = (uint32_t)(seen >> (kb * 32)) >> (g * 4);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int j = kb * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
-                        const bool see = x0 + j < x_end && (held >> j & 1) && sees(pos, t.keys.key(x0 + j), a.window, a.sinks);
-                        s[kb][v] = see ? s[kb][v] : -INFINITY;
-                    }
+                    for (int v = 0; v < 16; ++v) s[kb][v] = mine & (1u << ((v >> 2) * 8 + (v & 3))) ? s[kb][v] : -INFINITY;
                 }
             }
             float m = s[0][0];
@@ -241,10 +237,11 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
 #pragma unroll
                     for (int v = 0; v < 16; ++v) o[e][v] *= f;
             }
-            const bool odd = BITS == 16 && !plain && uniform(odd_step[wk][buffer]) == n;
+            const bool odd = BITS == 16 && !PLAIN && uniform(odd_step[wk][buffer]) == n;
             if (odd) {
+#pragma unroll 1
                 for (int j = 0; j < KT; ++j) {
-                    const bool see = x0 + j < x_end && (held >> j & 1) && sees(pos, t.keys.key(x0 + j), a.window, a.sinks);
+                    const bool see = seen >> j & 1;
 #pragma unroll
                     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -289,11 +286,20 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + e * 32)));
                         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + 8 * VS + e * 32)));
                         u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
-                        if (BITS == 16 && odd) vf = without_odd<BF>(vf);
+                        if (BITS == 16 && !PLAIN && odd) vf = without_odd<BF>(vf);
                         o[e] = product<MBF>(vf, pf, o[e]);
                     }
                 }
             }
+        };
+        if (!none) {
+            const uint64_t held = __ballot(pages_now >= 0);   // bit j: the page of key j is there (KT 32: bits twice)
+            const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
+                               (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);
+            if (plain)
+                compute(std::true_type(), held);
+            else
+                compute(std::false_type(), held);
         }
         put_rows((n + 1) & 1, n + 1, pages_next);
         __syncthreads();
@@ -318,11 +324,12 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     }
     sum = pair_sum(across_32(sum));
     if constexpr (BITS == 16) top = top == -INFINITY ? top : top * a.scale;
-    const int64_t line = (int64_t)b.n_tokens * a.heads, plane = (int64_t)split * line;
+    const int64_t plane = (int64_t)split * b.n_tokens * a.heads;
     if constexpr (WK == 1) {
         if (wr * 32 + lr >= t.rows) return;
         const int64_t to_row = (int64_t)(t.first + token);
-        if (splits == 1) {
+        const int64_t in_plane = to_row * a.heads + q_head, at = plane + in_plane;
+        if (share.parts == 1) {
             const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
             uint16_t *out = (uint16_t *)a.out + to_row * a.out_stride + q_head * D + g * 4;
 #pragma unroll
@@ -333,17 +340,16 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                     *(u32x2 *)(out + e * 32 + v4 * 8) = w;
                 }
         } else {
-            const int64_t at = plane + to_row * a.heads + q_head;
-            float *out = partials + at * D + g * 4;
+            float *out = partials.sums + at * D + g * 4;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e)
 #pragma unroll
                 for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(out + e * 32 + v4 * 8) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
-            if (g == 0) {
-                float *ml = partials + (int64_t)splits * line * D + at * 2;
-                ml[0] = top;
-                ml[1] = sum;
-            }
+        }
+        if (splits > 1 && g == 0) {
+            partials.top_weight[at * 2] = top;
+            partials.top_weight[at * 2 + 1] = sum;
+            if (split == 0) partials.parts[in_plane] = share.parts;
         }
     } else {
         // the groups' results, over the staged steps
@@ -375,36 +381,36 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                 for (int j = 0; j < 4; ++j) v[j] += x[j] * f;
             }
             const int rr = t.row0 + r, tok = quotient(rr, a.group, group_recip), qh = head * a.group + rr - tok * a.group;
-            if (splits == 1) {
+            const int64_t in_plane = (int64_t)(t.first + tok) * a.heads + qh, to = plane + in_plane;
+            if (share.parts == 1) {
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
                 const u32x2 w = {cache_pair<BF>(v[0] * inv, v[1] * inv), cache_pair<BF>(v[2] * inv, v[3] * inv)};
                 *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + at) = w;
             } else {
-                const int64_t to = plane + (int64_t)(t.first + tok) * a.heads + qh;
-                *(float4v *)(partials + to * D + at) = v;
-                if (at == 0) {
-                    float *ml = partials + (int64_t)splits * line * D + to * 2;
-                    ml[0] = m;
-                    ml[1] = l;
-                }
+                *(float4v *)(partials.sums + to * D + at) = v;
+            }
+            if (splits > 1 && at == 0) {
+                partials.top_weight[to * 2] = m;
+                partials.top_weight[to * 2 + 1] = l;
+                if (split == 0) partials.parts[in_plane] = share.parts;
             }
         }
     }
 }
 
 template <int BITS, bool BF, int D>
-void launch_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+void launch_tiles(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
     const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, hr, sr, (int)cut.tiles, cut.splits, partials); };
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, hr, sr, (int)cut.tiles, cut.splits, cut.keys, partials); };
     if (cut.tile_rows == 64)
         go(cache_tiles_kernel<BITS, BF, D, 2, 2>);
     else
         go(cache_tiles_kernel<BITS, BF, D, 4, 1>);
 }
 template <bool BF, int D>
-void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+void launch_bits(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     if (a.bits == 16)
         launch_tiles<16, BF, D>(a, cut, partials, stream);
@@ -416,7 +422,7 @@ void launch_bits(const AttentionCall &a, const AttentionCut &cut, float *partial
 
 }  // namespace
 
-hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream)
+hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     if (a.d == 64)
         a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);

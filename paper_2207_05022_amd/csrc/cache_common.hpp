@@ -2,6 +2,7 @@
 // keys a tile of queries sees, and the launches behind the entry points of cache_api.hip.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 #include "sti_internal.hpp"
 #include "lane_ops.hpp"
 
@@ -117,6 +118,17 @@ __device__ inline bool sees(int pos, int key, int window, int sinks)
     return key <= pos && (window <= 0 || key > pos - window || key < sinks);
 }
 
+// Bit j of the result: the query at `pos` sees number x0 + j of its tile's keys (below x_end).  Keys grow with their numbers, so that what a query
+// sees is the numbers below `sinks` and those from the window's first to its own.
+__device__ inline uint64_t bits_below(int n) { return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1; }
+__device__ inline uint64_t seen_keys(const TileKeys &keys, int pos, int window, int sinks, int x0, int x_end)
+{
+    const int own = pos < keys.low ? min(pos + 1, keys.sinks) : keys.sinks + pos - keys.low + 1;   // numbers of keys up to pos
+    uint64_t seen = bits_below(min(own, x_end) - x0);
+    if (window > 0) seen &= bits_below(sinks - x0) | ~bits_below(keys.sinks + max(0, pos - window + 1 - keys.low) - x0);
+    return seen;
+}
+
 // ---- launches (cache_store.hip, cache_attention.hip) ----
 hipError_t launch_cache_append(const CacheView &c, const BatchView &b, int bits, int d, sti_dtype stored, const void *k, const void *v,
                                sti_dtype io, int64_t k_stride, int64_t v_stride, hipStream_t stream);
@@ -134,20 +146,45 @@ struct AttentionCall {
     void *out;
     int64_t q_stride, out_stride;
 };
-// How a call of these sizes is cut: the kernel's rows per tile, and over how many workgroups each tile's keys are split.
+// How a call of these sizes is cut: the kernel's rows per tile, and the keys that one workgroup takes of a tile (a multiple of 256).  A tile of
+// more keys has several workgroups, at most `splits`; how many is known on the device.
 struct AttentionCut {
-    int tile_rows, splits;
+    int tile_rows, splits, keys;
     int64_t tiles;        // bound
 };
 AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads, int64_t capacity, int window, int sinks);
-// partial results of `splits` planes: sums [splits][n_tokens * heads][d] and maxima and weights' sums [splits][n_tokens * heads][2]
+// A workgroup's share of its tile's keys: numbers begin .. end - 1.
+struct KeyShare {
+    int begin, end, parts;   // parts: shares of the tile, 1: the workgroup leaves the result itself
+};
+__device__ inline KeyShare key_share(const TileKeys &keys, int split, int per_split)
+{
+    KeyShare s;
+    s.parts = max(1, (keys.count + per_split - 1) / per_split);
+    s.begin = split * per_split;
+    s.end = min(keys.count, s.begin + per_split);
+    return s;
+}
+// Partial results where tiles may have several shares: sums [splits][n_tokens * heads][d], maxima and weights' sums [splits][n_tokens * heads][2],
+// and of each row how many shares there are.
 inline size_t partial_bytes(int64_t n_tokens, int heads, int d, int splits)
 {
-    return splits > 1 ? (size_t)splits * n_tokens * heads * (d + 2) * sizeof(float) : 0;
+    const size_t rows = (size_t)n_tokens * heads;
+    return splits > 1 ? rows * splits * (d + 2) * sizeof(float) + rows * sizeof(int32_t) : 0;
 }
-hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);
-hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);     // tile_rows 16 and 32
-hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, float *partials, hipStream_t stream);   // 64 and 128
-hipError_t launch_cache_join(const AttentionCall &a, int splits, const float *partials, hipStream_t stream);
+struct Partials {
+    float *sums, *top_weight;
+    int32_t *parts;
+};
+inline Partials partials_at(void *workspace, int64_t n_tokens, int heads, int d, int splits)
+{
+    const size_t rows = (size_t)n_tokens * heads;
+    float *sums = (float *)workspace;
+    return Partials{sums, sums + rows * splits * d, (int32_t *)(sums + rows * splits * (d + 2))};
+}
+hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream);
+hipError_t launch_cache_few(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream);     // tile_rows 16
+hipError_t launch_cache_tiles(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream);   // 64 and 128
+hipError_t launch_cache_join(const AttentionCall &a, int splits, const Partials &partials, hipStream_t stream);
 
 }  // namespace sti

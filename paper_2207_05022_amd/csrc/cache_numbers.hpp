@@ -36,12 +36,14 @@ __device__ inline cache_u32x4 numbers_of_bytes(uint32_t w0, uint32_t w1)
 // 8 codes of 4 bits in the order 0 4 1 5 2 6 3 7: 1.1 instructions each
 __device__ inline cache_u32x4 numbers_of_nibbles(uint32_t w)
 {
+    uint32_t base = 0x64006400u;
+    asm("" : "+v"(base));   // (in a vector register: an instruction takes one constant from elsewhere, and and-or has two)
     cache_u32x4 out;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t v = i ? w >> 8 : w;
-        out[2 * i] = pair_minus((v & 0x000F000Fu) | 0x64006400u, 0x64086408u);                        // 1024 + 8
-        out[2 * i + 1] = pair_scaled((v & 0x00F000F0u) | 0x64006400u, 0x2C002C00u, 0xD480D480u);     // (1024 + 16 code) / 16 - (64 + 8)
+        out[2 * i] = pair_minus((v & 0x000F000Fu) | base, 0x64086408u);                        // 1024 + 8
+        out[2 * i + 1] = pair_scaled((v & 0x00F000F0u) | base, 0x2C002C00u, 0xD480D480u);     // (1024 + 16 code) / 16 - (64 + 8)
     }
     return out;
 }
