@@ -3,8 +3,9 @@
 //
 //   t_j = c s_k[j] (q . code_k[j]) + log2 s_v[j],   P_j = 2^(t_j - m),   o = sum_j P_j code_v[j] / sum_j P_j / s_v[j]
 //
-// (16 bits: s_k = s_v = 1).  Codes are exact in 16 bits, so that the only rounding in front of the matrix cores is that of the weights, and a
-// value's scale takes part in the maximum, so that a weight is largest where the value it carries is.
+// (16 bits: s_k = s_v = 1).  Codes are exact in binary16 (cache_numbers.hpp: with an offset that the sums lose again), so that the only
+// rounding in front of the matrix cores is that of the weights, and a value's scale takes part in the maximum, so that a weight is
+// largest where the value it carries is.
 //
 // A wave walks the keys KT at a time by itself, 16 queries in the columns of the products: S^T = K Q^T takes a key's row from memory as it lies,
 // a quarter of it to each group of 16 lanes (the queries' features in the same order), O^T = V^T P^T takes the weights from the registers of
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                                                               int per_split, Partials partials)
 {
     using T = FewShape<BITS, D, W>;
-    constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16, NQ = 1, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
+    constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
     constexpr bool MBF = BITS == 16 && BF;   // the products' type
     __shared__ __attribute__((aligned(16))) unsigned char lds[T::LDS];
     __shared__ float tops[T::HALF][ROWS], weights[T::HALF][ROWS];
@@ -76,13 +77,12 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
     uint32_t row = 0;
     uint64_t held = 0;
     auto key_of = [&](int x) { return t.keys.key(min(x + (lane & (KT - 1)), x_end - 1)); };
-    auto ask_pages = [&](int x) {
-        if (x < x_end) page = cache_page(c, b, t.seq, key_of(x));
-    };
+    auto ask_pages = [&](int x) { page = cache_page(c, b, t.seq, key_of(x)); };
     u32x4 kr[NKB][KP], vr[VP];
+    auto v_row = [&](int i) { return (i * 64 + lane) / (T::ROW / PIECE); };              // key and byte of the lane's piece i of a step's values
+    auto v_at = [&](int i) { return (i * 64 + lane) % (T::ROW / PIECE) * PIECE; };
     float scale = 0.f, scale_v = 0.f;
-    auto ask_rows = [&](int x) {
-        if (x >= x_end) return;
+    auto ask_rows = [&](int x) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
         held = __ballot(page >= 0);
         row = cache_row(c, max(page, 0), head, key_of(x));
 #pragma unroll
@@ -102,9 +102,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
         }
 #pragma unroll
         for (int i = 0; i < VP; ++i) {
-            constexpr int PER_ROW = T::ROW / PIECE;
-            const int item = i * 64 + lane, j = item / PER_ROW, at = item % PER_ROW * PIECE;
-            const uint8_t *src = c.v + (uint64_t)(uint32_t)__shfl((int)row, j) * T::ROW + at;
+            const uint8_t *src = c.v + (uint64_t)(uint32_t)__shfl((int)row, v_row(i)) * T::ROW + v_at(i);
             if constexpr (PIECE == 8) {
                 const u32x2 h = *(const u32x2 *)src;
                 vr[i] = u32x4{h.x, h.y, 0, 0};
@@ -118,161 +116,129 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
         }
     };
 
-    ask_pages(x0);
+    const bool some = x_end > share.begin;
+    if (some) ask_pages(x0);
 
     // queries as the B operand of S^T = K Q^T, features in the order of the keys' registers
-    u32x4 qf[NQ][D / 32];
-    int pos[NQ];
-    float back[NQ];   // what the scores of rows brought into binary16's range are multiplied by
+    const int q_row = t.row0 + min(lq, t.rows - 1), token = quotient(q_row, a.group, group_recip), q_head = head * a.group + q_row - token * a.group;
+    const int pos = t.base + token;
+    u32x4 qf[D / 32];
+    {
+        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * VALUES;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int r = t.row0 + min(n * 16 + lq, t.rows - 1), token = quotient(r, a.group, group_recip);
-        pos[n] = t.base + token;
-        back[n] = 1.f;
-        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + (head * a.group + r - token * a.group) * D + g * VALUES;
+        for (int i = 0; i < D / 32; ++i) qf[i] = *(const u32x4 *)(src + i * 8 / VALUES * 4 * VALUES + i * 8 % VALUES);
+    }
+    float4v offset = {0.f, 0.f, 0.f, 0.f};   // sums to start from: minus the queries times what the raw codes have too much
+    float key_factor = a.scale;              // what a key's sums are multiplied by, beside its scale, to be its scores
+    if constexpr (BITS < 16) {
+        // the same power of two for all queries of the wave
+        float most = four_max(largest_finite<D / 32, BF>(qf));
+        most = fmaxf(most, rotated<8>(most));
+        most = fmaxf(most, rotated<4>(most));
+        most = fmaxf(most, rotated<2>(most));
+        most = fmaxf(most, rotated<1>(most));
+        const int shift = query_shift<BITS == 8 ? 14 : 10>(most);
+        const float into = two_to(-shift);
+        key_factor *= two_to(shift + (BITS == 8 ? 24 : 20));
+        float total = 0.f;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) qf[n][s] = *(const u32x4 *)(src + s * 8 / VALUES * 4 * VALUES + s * 8 % VALUES);
-        if constexpr (BITS < 16 && BF) {
-            const int shift = query_shift(four_max(largest_magnitude(qf[n])));
-            bring_into_binary16(qf[n], shift);
-            back[n] = two_to(shift);
+        for (int s = 0; s < D / 32; ++s) {
+            if constexpr (BITS == 4) qf[s] = in_nibble_order(qf[s]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float by = BITS == 4 && !(i & 1) ? into * 16.f : into, too_much = BITS == 8 ? 128.f * 0x1p-24f : (i & 1 ? 128.f : 8.f) * 0x1p-24f;
+                const uint32_t p = qf[s][i], w = f16_pair_bits(cache_number<BF>(p & 0xFFFFu) * by, cache_number<BF>(p >> 16) * by);
+                qf[s][i] = w;
+                total += (cache_number<false>(w & 0xFFFFu) + cache_number<false>(w >> 16)) * too_much;
+            }
         }
-        if constexpr (BITS == 4)
-#pragma unroll
-            for (int s = 0; s < D / 32; ++s) qf[n][s] = in_nibble_order(qf[n][s]);
+        total = -four_sum(total);
+        offset = float4v{total, total, total, total};
     }
 
-    float4v o[NQ][D / 16];
-    float top[NQ], sum[NQ];   // (16 bits: top in units of the unscaled scores; sum: of this lane's keys)
+    float4v o[D / 16];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        top[n] = -INFINITY;
-        sum[n] = 0.f;
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) o[n][e] = float4v{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int e = 0; e < D / 16; ++e) o[e] = float4v{0.f, 0.f, 0.f, 0.f};
+    float4v extra = {0.f, 0.f, 0.f, 0.f};   // what the raw codes of the values add to every feature: O^T's row of a feature of such ones
+    float top = -INFINITY, sum = 0.f;       // (16 bits: top in units of the unscaled scores; sum: of this lane's keys)
 
     unsigned char *stage = lds + wave * T::STAGE;
     float *sc = (float *)(stage + KT * VS);
-    ask_rows(x0);
-    ask_pages(x0 + x_stride);
-    uint64_t held_now = 0;
-    // whether every query sees every key of the step at x0
-    auto seen_by_all = [&]() {
+    if (some) {
+        ask_rows(x0);
+        ask_pages(x0 + x_stride);
+    }
+    // (one way through a step, branches around what few steps need: registers that two ways leave in different places are copied, and requests on
+    // their way waited for)
+    for (; x0 < x_end; x0 += x_stride) {
+        const uint64_t held_now = held;
+        // whether every query sees every key of the step
         const int key_first = t.keys.key(x0), key_last = t.keys.key(x0 + KT - 1);
-        return x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= t.first_pos &&
-               (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);
-    };
-    auto compute = [&](auto all_see) {
-        constexpr bool PLAIN = decltype(all_see)::value;
-        held_now = held;
-        float4v s[NQ][NKB];
+        const bool plain = x0 + KT <= x_end && held_now == ~(uint64_t)0 && key_last <= t.first_pos &&
+                           (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);
+        float4v s[NKB];
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) s[n][kb] = float4v{0.f, 0.f, 0.f, 0.f};
+            s[kb] = offset;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
                 u32x4 kf;
                 if constexpr (BITS == 16)
                     kf = kr[kb][i];
                 else if constexpr (BITS == 8)
-                    kf = numbers_of_bytes(kr[kb][i / 2][(i & 1) * 2], kr[kb][i / 2][(i & 1) * 2 + 1]);
+                    kf = raw_bytes(kr[kb][i / 2][(i & 1) * 2], kr[kb][i / 2][(i & 1) * 2 + 1]);
                 else
-                    kf = numbers_of_nibbles(kr[kb][0][i]);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) s[n][kb] = product<MBF>(kf, qf[n][i], s[n][kb]);
+                    kf = raw_nibbles(kr[kb][0][i]);
+                s[kb] = product<MBF>(kf, qf[i], s[kb]);
             }
         }
         uint32_t odd = 0;
+        if constexpr (BITS == 16)
+            if (!plain)
 #pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            constexpr int PER_ROW = T::ROW / PIECE;
-            const int item = i * 64 + lane, j = item / PER_ROW, at = item % PER_ROW * PIECE;
-            if constexpr (PIECE == 8)
-                *(u32x2 *)(stage + j * VS + at) = u32x2{vr[i][0], vr[i][1]};
-            else
-                *(u32x4 *)(stage + j * VS + at) = vr[i];
-            if constexpr (BITS == 16 && !PLAIN)
+                for (int i = 0; i < VP; ++i)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) odd |= odd_halves<BF>(vr[i][w]);
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            if constexpr (PIECE == 8)
+                *(u32x2 *)(stage + v_row(i) * VS + v_at(i)) = u32x2{vr[i][0], vr[i][1]};
+            else
+                *(u32x4 *)(stage + v_row(i) * VS + v_at(i)) = vr[i];
         }
-        const bool some_odd = BITS == 16 && !PLAIN && __any(odd != 0);
         if constexpr (BITS < 16) {
             if (lane < KT) {
                 const ValueScale v = value_scale(scale_v);
-                sc[lane] = scale * a.scale;
+                sc[lane] = scale * key_factor;
                 sc[KT + lane] = v.log;
-                sc[2 * KT + lane] = v.inverse;
+                sc[2 * KT + lane] = BITS == 4 && !(lane & 1) ? v.inverse * 0.0625f : v.inverse;
             }
         }
         wave_lds_fence();
+        // the registers of this step's rows are free: the next ones' requests may not move in front of their last use (they would go to other
+        // registers)
+        __builtin_amdgcn_sched_barrier(0);
         ask_rows(x0 + x_stride);
         ask_pages(x0 + 2 * x_stride);
 
-        uint32_t pk[NQ][NKB / 2][4];   // the weights, 16 bits, in the order of V^T's registers
+        if constexpr (BITS < 16) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            if constexpr (BITS < 16) {
+            for (int kb = 0; kb < NKB; ++kb) {
+                const int at = g * 4 * NKB + kb * 4;
+                const float4v k4 = *(const float4v *)(sc + at), l4 = *(const float4v *)(sc + KT + at);
 #pragma unroll
-                for (int kb = 0; kb < NKB; ++kb) {
-                    const int at = g * 4 * NKB + kb * 4;
-                    const float4v k4 = *(const float4v *)(sc + at), l4 = *(const float4v *)(sc + KT + at);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) s[n][kb][v] = fmaf(BF ? s[n][kb][v] * back[n] : s[n][kb][v], k4[v], l4[v]);
-                }
+                for (int v = 0; v < 4; ++v) s[kb][v] = fmaf(s[kb][v], k4[v], l4[v]);
             }
-            uint64_t seen = 0;
-            if constexpr (!PLAIN) {
-                seen = seen_keys(t.keys, pos[n], a.window, a.sinks, x0, x_end) & held_now;
-                const uint32_t mine = (uint32_t)(seen >> (g * 4 * NKB));
-#pragma unroll
-                for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) s[n][kb][v] = mine & (1u << (kb * 4 + v)) ? s[n][kb][v] : -INFINITY;
-            }
-            float m = s[n][0][0];
+        }
+        if (!plain) {
+            const uint64_t seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held_now;
+            const uint32_t mine = (uint32_t)(seen >> (g * 4 * NKB));
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) m = fmaxf(m, s[n][kb][v]);
-            m = four_max(m);
-            // a query's results are shrunk only where its maximum has grown by more than 2^8: weights up to 256 are as exact as those up to 1
-            const float factor = BITS == 16 ? a.scale : 1.f;
-            const bool grown = (m - top[n]) * factor > 8.f || (top[n] == -INFINITY && m > -INFINITY);
-            if (__any(grown)) {
-                const float f = grown ? __builtin_amdgcn_exp2f((top[n] - m) * factor) : 1.f;
-                top[n] = grown ? m : top[n];
-                sum[n] *= f;
-#pragma unroll
-                for (int e = 0; e < D / 16; ++e)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) o[n][e][v] *= f;
-            }
-            const float shift = top[n] == -INFINITY ? 0.f : -top[n] * factor;
-            float p[NKB][4];
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) p[kb][v] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(s[n][kb][v], factor, shift) : s[n][kb][v] + shift);
-                if constexpr (BITS == 16) {
-                    sum[n] += (p[kb][0] + p[kb][1]) + (p[kb][2] + p[kb][3]);
-                } else {
-                    const float4v i4 = *(const float4v *)(sc + 2 * KT + g * 4 * NKB + kb * 4);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) sum[n] = fmaf(p[kb][v], i4[v], sum[n]);
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < NKB / 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (BITS == 4)   // the order of numbers_of_nibbles
-                        pk[n][h][i] = cache_pair<false>(p[2 * h][i], p[2 * h + 1][i]);
-                    else
-                        pk[n][h][i] = cache_pair<MBF>(p[2 * h + (i >> 1)][(i & 1) * 2], p[2 * h + (i >> 1)][(i & 1) * 2 + 1]);
-                }
-            if (some_odd) {
+                for (int v = 0; v < 4; ++v) s[kb][v] = mine & (1u << (kb * 4 + v)) ? s[kb][v] : -INFINITY;
+            if (BITS == 16 && __any(odd != 0)) {
+                // values that are not finite: to the queries that see them, and out of the products' way
 #pragma unroll 1
                 for (int j = 0; j < KT; ++j) {
                     const bool see = seen >> j & 1;
@@ -282,14 +248,71 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
-                            if (bad & 1) o[n][e][2 * i] += cache_number<BF>(pair & 0xFFFFu);
-                            if (bad >> 31) o[n][e][2 * i + 1] += cache_number<BF>(pair >> 16);
+                            if (bad & 1) o[e][2 * i] += cache_number<BF>(pair & 0xFFFFu);
+                            if (bad >> 31) o[e][2 * i + 1] += cache_number<BF>(pair >> 16);
                         }
                     }
                 }
+                wave_lds_fence();
+#pragma unroll 1
+                for (int i = 0; i < VP; ++i) {
+                    u32x4 *at = (u32x4 *)(stage + v_row(i) * VS + v_at(i));
+                    *at = without_odd<BF>(*at);
+                }
+                wave_lds_fence();
             }
         }
+        float m = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) m = fmaxf(m, s[kb][v]);
+        m = four_max(m);
+        // a query's results are shrunk only where its maximum has grown by more than 2^8: weights up to 256 are as exact as those up to 1
+        const float factor = BITS == 16 ? a.scale : 1.f;
+        const bool grown = (m - top) * factor > 8.f || (top == -INFINITY && m > -INFINITY);
+        if (__any(grown)) {
+            const float f = grown ? __builtin_amdgcn_exp2f((top - m) * factor) : 1.f;
+            top = grown ? m : top;
+            sum *= f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) extra[v] *= f;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) o[e][v] *= f;
+        }
+        const float shift = top == -INFINITY ? 0.f : -top * factor;
+        float p[NKB][4];
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)   // (4 bits: 16 times as much beside the first and third pair of raw_nibbles)
+                p[kb][v] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(s[kb][v], factor, shift) : s[kb][v] + (BITS == 4 && !(v & 1) ? shift + 4.f : shift));
+            if constexpr (BITS == 16) {
+                sum += (p[kb][0] + p[kb][1]) + (p[kb][2] + p[kb][3]);
+            } else {
+                const float4v i4 = *(const float4v *)(sc + 2 * KT + g * 4 * NKB + kb * 4);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sum = fmaf(p[kb][v], i4[v], sum);
+            }
+        }
+        u32x4 pf[NKB / 2];   // the weights, 16 bits, in the order of V^T's registers
+#pragma unroll
+        for (int h = 0; h < NKB / 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (BITS == 4)   // the order of raw_nibbles
+                    pf[h][i] = cache_pair<false>(p[2 * h][i], p[2 * h + 1][i]);
+                else
+                    pf[h][i] = cache_pair<MBF>(p[2 * h + (i >> 1)][(i & 1) * 2], p[2 * h + (i >> 1)][(i & 1) * 2 + 1]);
+            }
         // O^T += V^T P^T
+        if constexpr (BITS < 16) {
+            const u32x4 too_much = BITS == 8 ? u32x4{0x00800080u, 0x00800080u, 0x00800080u, 0x00800080u} : u32x4{0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u};
+#pragma unroll
+            for (int h = 0; h < NKB / 2; ++h) extra = product<false>(too_much, pf[h], extra);
+        }
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
             if constexpr (BITS == 16) {
@@ -297,10 +320,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                 const unsigned char *src = stage + (g * 8 + (lq >> 2)) * VS + e * 32 + (lq & 3) * 8;
                 const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)src));
                 const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(src + 4 * VS)));
-                u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
-                if (!PLAIN && some_odd) vf = without_odd<BF>(vf);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) o[n][e] = product<MBF>(vf, u32x4{pk[n][0][0], pk[n][0][1], pk[n][0][2], pk[n][0][3]}, o[n][e]);
+                o[e] = product<MBF>(u32x4{lo.x, lo.y, hi.x, hi.y}, pf[0], o[e]);
             } else {
                 typedef __attribute__((address_space(3))) int2v *LdsInt2;
                 const unsigned char *src = BITS == 8 ? stage + (g * 8 + (lq >> 1)) * VS + e * 16 + (lq & 1) * 8 : stage + (g * 16 + lq) * VS + e * 8;
@@ -311,88 +331,64 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
                     w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((LdsInt2)src);
                 const uint32_t w0 = (uint32_t)w.x, w1 = (uint32_t)w.y;
 #pragma unroll
-                for (int h = 0; h < NKB / 2; ++h) {
-                    const u32x4 vf = BITS == 8 ? numbers_of_bytes(w0, w1) : numbers_of_nibbles(h ? w1 : w0);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][e] = product<false>(vf, u32x4{pk[n][h][0], pk[n][h][1], pk[n][h][2], pk[n][h][3]}, o[n][e]);
-                }
+                for (int h = 0; h < NKB / 2; ++h) o[e] = product<false>(BITS == 8 ? raw_bytes(w0, w1) : raw_nibbles(h ? w1 : w0), pf[h], o[e]);
             }
         }
         wave_lds_fence();
-    };
-    // (loops of their own: what two paths leave in registers would be copied where they meet)
-    while (x0 < x_end) {
-        while (x0 < x_end && seen_by_all()) {
-            compute(std::true_type());
-            x0 += x_stride;
-        }
-        if (x0 < x_end) {
-            compute(std::false_type());
-            x0 += x_stride;
-        }
     }
 
-    // join the waves: the upper half leaves its results in LDS, the lower half adds them, until one is left
+    sum = four_sum(sum);
+    if constexpr (BITS == 16) top = top == -INFINITY ? top : top * a.scale;
+    if constexpr (BITS < 16)
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        sum[n] = four_sum(sum[n]);
-        if constexpr (BITS == 16) top[n] = top[n] == -INFINITY ? top[n] : top[n] * a.scale;
-    }
+        for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[e][v] = (o[e][v] - extra[v]) * (BITS == 8 ? 0x1p24f : 0x1p20f);
+
+    // join the waves: the upper half leaves its results in LDS, the lower half adds them, until one is left
     float *join = (float *)lds;
 #pragma unroll
     for (int half = W / 2; half >= 1; half /= 2) {
         __syncthreads();
         if (wave >= half && wave < 2 * half) {
+            float *to = join + ((wave - half) * ROWS + lq) * JS + g * 4;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float *to = join + ((wave - half) * ROWS + n * 16 + lq) * JS + g * 4;
-#pragma unroll
-                for (int e = 0; e < D / 16; ++e) *(float4v *)(to + e * 16) = o[n][e];
-                if (g == 0) {
-                    tops[wave - half][n * 16 + lq] = top[n];
-                    weights[wave - half][n * 16 + lq] = sum[n];
-                }
+            for (int e = 0; e < D / 16; ++e) *(float4v *)(to + e * 16) = o[e];
+            if (g == 0) {
+                tops[wave - half][lq] = top;
+                weights[wave - half][lq] = sum;
             }
         }
         __syncthreads();
         if (wave < half) {
+            const float theirs = tops[wave][lq], m = fmaxf(top, theirs);
+            const float f0 = top == m ? 1.f : __builtin_amdgcn_exp2f(top - m), f1 = theirs == m ? 1.f : __builtin_amdgcn_exp2f(theirs - m);
+            top = m;
+            sum = sum * f0 + weights[wave][lq] * f1;
+            const float *from = join + (wave * ROWS + lq) * JS + g * 4;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                const float theirs = tops[wave][n * 16 + lq], m = fmaxf(top[n], theirs);
-                const float f0 = top[n] == m ? 1.f : __builtin_amdgcn_exp2f(top[n] - m), f1 = theirs == m ? 1.f : __builtin_amdgcn_exp2f(theirs - m);
-                top[n] = m;
-                sum[n] = sum[n] * f0 + weights[wave][n * 16 + lq] * f1;
-                const float *from = join + (wave * ROWS + n * 16 + lq) * JS + g * 4;
+            for (int e = 0; e < D / 16; ++e) {
+                const float4v x = *(const float4v *)(from + e * 16);
 #pragma unroll
-                for (int e = 0; e < D / 16; ++e) {
-                    const float4v x = *(const float4v *)(from + e * 16);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) o[n][e][v] = o[n][e][v] * f0 + x[v] * f1;
-                }
+                for (int v = 0; v < 4; ++v) o[e][v] = o[e][v] * f0 + x[v] * f1;
             }
         }
     }
-    if (wave != 0) return;
+    if (wave != 0 || lq >= t.rows) return;
+    const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, plane = (int64_t)split * b.n_tokens * a.heads + to_row;
+    if (share.parts == 1) {
+        const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+        uint16_t *out = (uint16_t *)a.out + (t.first + token) * a.out_stride + q_head * D + g * 4;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        if (n * 16 + lq >= t.rows) continue;
-        const int r = t.row0 + n * 16 + lq, token = quotient(r, a.group, group_recip), q_head = head * a.group + r - token * a.group;
-        const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, plane = (int64_t)split * b.n_tokens * a.heads + to_row;
-        if (share.parts == 1) {
-            const float inv = sum[n] > 0.f ? 1.0f / sum[n] : (sum[n] == 0.f ? 0.f : sum[n]);
-            uint16_t *out = (uint16_t *)a.out + (t.first + token) * a.out_stride + q_head * D + g * 4;
+        for (int e = 0; e < D / 16; ++e) *(u32x2 *)(out + e * 16) = u32x2{cache_pair<BF>(o[e][0] * inv, o[e][1] * inv), cache_pair<BF>(o[e][2] * inv, o[e][3] * inv)};
+    } else {
 #pragma unroll
-            for (int e = 0; e < D / 16; ++e)
-                *(u32x2 *)(out + e * 16) = u32x2{cache_pair<BF>(o[n][e][0] * inv, o[n][e][1] * inv), cache_pair<BF>(o[n][e][2] * inv, o[n][e][3] * inv)};
-        } else {
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e) *(float4v *)(partials.sums + plane * D + g * 4 + e * 16) = o[n][e];
-        }
-        if (splits > 1 && g == 0) {
-            partials.top_weight[plane * 2] = top[n];
-            partials.top_weight[plane * 2 + 1] = sum[n];
-            if (split == 0) partials.parts[to_row] = share.parts;
-        }
+        for (int e = 0; e < D / 16; ++e) *(float4v *)(partials.sums + plane * D + g * 4 + e * 16) = o[e];
+    }
+    if (splits > 1 && g == 0) {
+        partials.top_weight[plane * 2] = top;
+        partials.top_weight[plane * 2 + 1] = sum;
+        if (split == 0) partials.parts[to_row] = share.parts;
     }
 }
 

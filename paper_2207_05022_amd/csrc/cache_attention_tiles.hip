@@ -70,15 +70,30 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     const int wave_last = t.row0 + min(wr * 32 + 31, t.rows - 1);
     const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, group_recip), last_pos = t.base + quotient(wave_last, a.group, group_recip);
     u32x4 qf[D / 16];
-    float back = 1.f;   // what the scores of a row brought into binary16's range are multiplied by
+    float back = 1.f;   // what the scores of queries brought into binary16's range are multiplied by
     {
         const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + s * 16);
         if constexpr (BITS < 16 && BF) {
-            const int shift = query_shift(pair_max(across_32(largest_magnitude(qf))));
-            bring_into_binary16(qf, shift);
+            // binary16 beside codes: all queries of the wave by one power of two
+            float most = pair_max(across_32(largest_finite<D / 16, BF>(qf)));
+            most = pair_max(across_16(most));
+            most = fmaxf(most, rotated<8>(most));
+            most = fmaxf(most, rotated<4>(most));
+            most = fmaxf(most, rotated<2>(most));
+            most = fmaxf(most, rotated<1>(most));
+            const int shift = query_shift<14>(most);
+            const float into = two_to(-shift);
             back = two_to(shift);
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t p = qf[s][i];
+                    qf[s][i] = f16_pair_bits(cache_number<BF>(p & 0xFFFFu) * into, cache_number<BF>(p >> 16) * into);
+                }
+            }
         }
         if constexpr (BITS == 4)
 #pragma unroll
@@ -102,10 +117,9 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     int pages = -1, pages_now = -1;   // of key `lane` % KT of a step
     auto ask_pages = [&](int x0) {
         const int x = x0 + (lane & (KT - 1));
-        if (x0 < x_end) pages = cache_page(c, b, t.seq, t.keys.key(min(x, x_end - 1)));
+        pages = cache_page(c, b, t.seq, t.keys.key(min(x, x_end - 1)));
     };
-    auto ask_rows = [&](int x0) {
-        if (x0 >= x_end) return;
+    auto ask_rows = [&](int x0) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
         const uint32_t of_key = cache_row(c, max(pages, 0), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));   // row of key `lane` % KT
 #pragma unroll
         for (int i = 0; i < T::ITEMS; ++i) {
@@ -173,11 +187,13 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     if (lane == 0)
         for (int i = 0; i < T::BUFFERS; ++i) odd_step[wk][i] = -1;   // (the waves of a group write the same; a find comes behind the barrier)
     __syncthreads();
-    ask_pages(x_first);
-    ask_rows(x_first);
-    pages_now = pages;
-    ask_pages(x_first + x_stride);
-    put_rows(0, 0, pages_now);
+    if (rounds > 0) {
+        ask_pages(x_first);
+        ask_rows(x_first);
+        pages_now = pages;
+        ask_pages(x_first + x_stride);
+        put_rows(0, 0, pages_now);
+    }
     __syncthreads();
     for (int n = 0; n < rounds; ++n) {
         const int x0 = x_first + n * x_stride, buffer = n & 1;
