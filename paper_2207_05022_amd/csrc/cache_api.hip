@@ -128,7 +128,7 @@ size_t sti_cache_attention_workspace_bytes(const sti_cache *cache, const sti_cac
 {
     if (check_cache(cache) != STI_OK || check_batch(*cache, batch) != STI_OK || !valid_heads(*cache, *batch, n_heads)) return 0;
     if (window < 0 || sinks < 0 || batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
-    return partial_bytes(batch->n_tokens, n_heads, cache->d_head, cut_of(*cache, *batch, n_heads, window, sinks).splits);
+    return partial_bytes(cut_of(*cache, *batch, n_heads, window, sinks), batch->n_tokens, n_heads, cache->d_head);
 }
 
 sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *batch, const void *q, void *out, sti_dtype io_dtype,
@@ -148,10 +148,10 @@ sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *ba
     if (st == STI_OK) st = check_rows(out, out_stride, (int64_t)n_heads * cache->d_head, io_dtype);
     if (st != STI_OK) return st;
     const AttentionCut cut = cut_of(*cache, *batch, n_heads, window, sinks);
-    const size_t need = partial_bytes(batch->n_tokens, n_heads, cache->d_head, cut.splits);
+    const size_t need = partial_bytes(cut, batch->n_tokens, n_heads, cache->d_head);
     if (need && (!workspace || workspace_bytes < need)) return STI_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16)) return STI_ERR_ALIGN;
-    if (cut.tiles * cut.splits * cache->n_kv_heads > kMostBlocks) return STI_ERR_DIMS;
+    if (cut.blocks > kMostBlocks) return STI_ERR_DIMS;
     AttentionCall a;
     a.cache = view(*cache);
     a.batch = view(*batch);
@@ -168,10 +168,10 @@ sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *ba
     a.out = out;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    const Partials partials = partials_at(workspace, batch->n_tokens, n_heads, cache->d_head, cut.splits);
+    const Partials partials = partials_at(workspace, cut, cache->d_head);
     st = timed_call(STI_K_ATTENTION, [&] { return launch_cache_attention(a, cut, partials, (hipStream_t)hip_stream); });
-    if (st != STI_OK || cut.splits == 1) return st;
-    return timed_call(STI_K_ATTENTION, [&] { return launch_cache_join(a, cut.splits, partials, (hipStream_t)hip_stream); });
+    if (st != STI_OK || cut.work.slots == 0) return st;
+    return timed_call(STI_K_ATTENTION, [&] { return launch_cache_join(a, cut, partials, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"

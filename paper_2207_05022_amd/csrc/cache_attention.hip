@@ -89,8 +89,7 @@ __device__ inline uint16_t rounded(float v)
 
 // ROWS (token, head) pairs of one key/value head per workgroup
 template <int BITS, bool BF, int D, int ROWS>
-__global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip,
-                                                                      int splits, int per_split, Partials partials)
+__global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionCall a, WorkCut cut, Partials partials)
 {
     using P = Piece<BITS>;
     constexpr int VALUES = P::VALUES, LPK = D / VALUES, AT_ONCE = 64 / LPK, U = 4, STEP = AT_ONCE * U, ROW_BYTES = D * BITS / 8;
@@ -99,19 +98,15 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), part = lane % LPK, group_lane = lane / LPK;
     const CacheView &c = a.cache;
     const BatchView &b = a.batch;
-    // blocks in the order (tile, split, head)
-    const int tile_split = quotient(blockIdx.x, c.heads, heads_recip), head = blockIdx.x - tile_split * c.heads;
-    const int tile = quotient(tile_split, splits, splits_recip), split = tile_split - tile * splits;
-    const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
+    const int from_last = quotient(blockIdx.x, c.heads, cut.heads_recip), head = blockIdx.x - from_last * c.heads;   // blocks in the order (item, head)
+    const QueryTile t = find_work(c, b, cut, from_last, head, a.group, a.window, a.sinks);
     if (t.seq < 0) return;
-    const KeyShare share = key_share(t.keys, split, per_split);
-    if (split >= share.parts) return;
 
     float q[ROWS][VALUES], o[ROWS][VALUES], top[ROWS], sum[ROWS];
     int pos[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        const int row = t.row0 + min(r, t.rows - 1), token = quotient(row, a.group, group_recip);
+        const int row = t.row0 + min(r, t.rows - 1), token = quotient(row, a.group, cut.group_recip);
         pos[r] = t.base + token;
         const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + (head * a.group + row - token * a.group) * D + part * VALUES;
 #pragma unroll
@@ -127,8 +122,8 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
         sum[r] = 0.f;
     }
 
-    const int x_end = share.end;
-    for (int x0 = share.begin + wave * STEP; x0 < x_end; x0 += kWaves * STEP) {
+    const int x_end = t.end;
+    for (int x0 = t.begin + wave * STEP; x0 < x_end; x0 += kWaves * STEP) {
         P k[U], v[U];
         float ks[U], vs[U];
         int key[U];
@@ -219,18 +214,17 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
             l += weights[j][r] * f;
             w += sums[j][r][at] * f;
         }
-        const int row = t.row0 + r, token = quotient(row, a.group, group_recip);
+        const int row = t.row0 + r, token = quotient(row, a.group, cut.group_recip);
         const int q_head = head * a.group + row - token * a.group;
-        if (share.parts == 1) {
+        const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, place = (t.slot + (int64_t)t.split * c.heads) * ROWS + r;
+        if (t.parts == 1)
             ((uint16_t *)a.out)[(t.first + token) * a.out_stride + q_head * D + at] = rounded<BF>(l > 0.f ? w / l : (l == 0.f ? 0.f : l));
-            if (splits == 1) continue;
-        }
-        const int64_t line = (int64_t)b.n_tokens * a.heads, to_row = (int64_t)(t.first + token) * a.heads + q_head, plane = (int64_t)split * line + to_row;
-        if (share.parts > 1) partials.sums[plane * D + at] = w;
-        if (at == 0) {
-            partials.top_weight[plane * 2] = m;
-            partials.top_weight[plane * 2 + 1] = l;
-            if (split == 0) partials.parts[to_row] = share.parts;
+        else
+            partials.sums[place * D + at] = w;
+        if (cut.slots > 0 && at == 0) {
+            partials.top_weight[place * 2] = m;
+            partials.top_weight[place * 2 + 1] = l;
+            if (t.split == 0) partials.rows[to_row] = {(int32_t)place, t.parts};
         }
     }
 }
@@ -238,7 +232,7 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
 // The splits' results, each shrunk to the largest maximum.  D / 4 threads of 4 features take a row's splits GROUPS at a time; the groups of a row
 // are joined through LDS.
 template <bool BF, int D, int GROUPS>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32_t heads_recip, Partials partials)
+__global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32_t heads_recip, int tile_rows, Partials partials)
 {
     constexpr int WIDE = D / 4, PER_ROW = WIDE * GROUPS, ROWS = 256 / PER_ROW;
     __shared__ float4v sums[GROUPS > 1 ? GROUPS : 1][WIDE];
@@ -248,16 +242,18 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32
     const int row = (int)(blockIdx.x * ROWS + threadIdx.x / PER_ROW), group = threadIdx.x / WIDE % GROUPS, at = threadIdx.x % WIDE;
     if (row >= line) return;   // (rows are whole blocks where groups meet, here and below)
     const int token = quotient(row, a.heads, heads_recip), head = row - token * a.heads;
-    const int first = b.offsets[0], end = b.offsets[b.n_seqs], parts = partials.parts[row];
+    const int first = b.offsets[0], end = b.offsets[b.n_seqs];
+    const RowShares shares_of = partials.rows[row];
+    const int parts = shares_of.parts;
     if (token < first || token >= end || parts == 1) return;   // (of no sequence: no tile has left anything; one share: it has left the result)
     const float2v *ml = (const float2v *)partials.top_weight;
     float m = -INFINITY, l = 0.f;
     float4v w = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = group; s < parts; s += GROUPS) {
-        const int64_t plane = (int64_t)s * line + row;
-        const float2v theirs = ml[plane];
-        const float4v x = *(const float4v *)(partials.sums + plane * D + at * 4);
+        const int64_t place = shares_of.place + (int64_t)s * a.cache.heads * tile_rows;
+        const float2v theirs = ml[place];
+        const float4v x = *(const float4v *)(partials.sums + place * D + at * 4);
         const float t = fmaxf(m, theirs.x), f0 = factor(m, t), f1 = factor(theirs.x, t);
         m = t;
         l = l * f0 + theirs.y * f1;
@@ -290,9 +286,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32
 template <int BITS, bool BF, int D>
 void launch_rows(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
-    const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    launch(cache_attention_kernel<BITS, BF, D, 1>, grid, dim3(kWaves * 64), 0, stream, a, gr, hr, sr, cut.splits, cut.keys, partials);
+    launch(cache_attention_kernel<BITS, BF, D, 1>, dim3((uint32_t)cut.blocks), dim3(kWaves * 64), 0, stream, a, cut.work, partials);
 }
 template <bool BF, int D>
 void launch_bits(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
@@ -313,21 +307,24 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     // rows that share a key/value head in an average sequence
     const int64_t rows = (n_tokens + n_seqs - 1) / n_seqs * group;
     AttentionCut cut;
-    cut.tile_rows = rows <= 1 ? 1 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
-    cut.tiles = tile_bound(n_tokens, n_seqs, group, cut.tile_rows);
-    int64_t keys = capacity;   // the most that a tile's queries see (its tokens: at most tile_rows of them)
-    if (window > 0) keys = std::min(keys, (int64_t)window + sinks + cut.tile_rows);
-    // fewer than two workgroups to a compute unit: shares of the keys for four
-    const int64_t blocks = cut.tiles * kv_heads, parts = blocks < 512 ? (1024 + blocks - 1) / blocks : 1;
-    cut.keys = (int)std::max<int64_t>(512, ((keys + parts - 1) / parts + 255) / 256 * 256);
-    cut.splits = (int)std::max<int64_t>(1, (keys + cut.keys - 1) / cut.keys);
+    WorkCut &w = cut.work;
+    w.rows = rows <= 1 ? 1 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    w.token_rows = (w.rows + group - 2) / group + 1;   // (a tile may begin and end inside a token's heads)
+    w.group_recip = reciprocal((uint32_t)group);
+    w.heads_recip = reciprocal((uint32_t)kv_heads);
+    w.least_keys = 256;
+    int64_t keys = capacity;   // the most that a tile's queries see
+    if (window > 0) keys = std::min(keys, (int64_t)window + sinks + w.token_rows);
+    const int64_t tiles = tile_bound(n_tokens, n_seqs, group, w.rows), slots = (w.rows == 1 ? 1024 : 512) / kv_heads;
+    w.slots = tiles * kv_heads < 512 && keys >= 2 * w.least_keys ? (int32_t)slots : 0;
+    cut.blocks = (w.slots > 0 ? slots : tiles) * kv_heads;
     return cut;
 }
 
 hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
-    if (cut.tile_rows > 16) return launch_cache_tiles(a, cut, partials, stream);
-    if (cut.tile_rows > 1) return launch_cache_few(a, cut, partials, stream);
+    if (cut.work.rows > 16) return launch_cache_tiles(a, cut, partials, stream);
+    if (cut.work.rows > 1) return launch_cache_few(a, cut, partials, stream);
     if (a.d == 64)
         a.bf16 ? launch_bits<true, 64>(a, cut, partials, stream) : launch_bits<false, 64>(a, cut, partials, stream);
     else
@@ -335,15 +332,15 @@ hipError_t launch_cache_attention(const AttentionCall &a, const AttentionCut &cu
     return hipGetLastError();
 }
 
-hipError_t launch_cache_join(const AttentionCall &a, int splits, const Partials &partials, hipStream_t stream)
+hipError_t launch_cache_join(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.batch.n_tokens * a.heads;
     const uint32_t recip = reciprocal((uint32_t)a.heads);
-    // many rows: each to D / 4 threads; few (many splits, then): each to a workgroup
-    const bool many = rows < 2048 && splits > 4;
+    // many rows: each to D / 4 threads; few (many shares, then): each to a workgroup
+    const bool many = rows < 2048;
     const int64_t threads = many ? 256 : a.d / 4;
     const dim3 grid((uint32_t)((rows * threads + 255) / 256));
-    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, recip, partials); };
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, recip, cut.work.rows, partials); };
     if (a.d == 64) {
         if (a.bf16)
             many ? go(cache_join_kernel<true, 64, 16>) : go(cache_join_kernel<true, 64, 1>);

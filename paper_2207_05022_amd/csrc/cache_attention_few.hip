@@ -50,8 +50,7 @@ struct FewShape {
 
 // 16 queries of one key/value head, W waves
 template <int BITS, bool BF, int D, int W>
-__global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int splits,
-                                                              int per_split, Partials partials)
+__global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, WorkCut cut, Partials partials)
 {
     using T = FewShape<BITS, D, W>;
     constexpr int KT = T::KT, NKB = T::NKB, ROWS = 16, KP = T::KP, VP = T::VP, PIECE = T::PIECE, VALUES = T::VALUES, VS = T::VS, JS = T::JS;
@@ -61,16 +60,11 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
     const CacheView &c = a.cache;
     const BatchView &b = a.batch;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, lq = lane & 15;
-    // blocks in the order (tile, split, head)
-    const int tile_split = quotient(blockIdx.x, c.heads, heads_recip), head = blockIdx.x - tile_split * c.heads;
-    const int tile = quotient(tile_split, splits, splits_recip), split = tile_split - tile * splits;
-    const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
+    const int from_last = quotient(blockIdx.x, c.heads, cut.heads_recip), head = blockIdx.x - from_last * c.heads;   // blocks in the order (item, head)
+    const QueryTile t = find_work(c, b, cut, from_last, head, a.group, a.window, a.sinks);
     if (t.seq < 0) return;
-
-    const KeyShare share = key_share(t.keys, split, per_split);
-    if (split >= share.parts) return;
-    const int x_end = share.end, x_stride = W * KT;
-    int x0 = share.begin + wave * KT;
+    const int x_end = t.end, x_stride = W * KT;
+    int x0 = t.begin + wave * KT;
 
     // row of key `lane` % KT of a step in the pool, and whether its page is there
     int page = -1;
@@ -116,11 +110,11 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
         }
     };
 
-    const bool some = x_end > share.begin;
+    const bool some = x_end > t.begin;
     if (some) ask_pages(x0);
 
     // queries as the B operand of S^T = K Q^T, features in the order of the keys' registers
-    const int q_row = t.row0 + min(lq, t.rows - 1), token = quotient(q_row, a.group, group_recip), q_head = head * a.group + q_row - token * a.group;
+    const int q_row = t.row0 + min(lq, t.rows - 1), token = quotient(q_row, a.group, cut.group_recip), q_head = head * a.group + q_row - token * a.group;
     const int pos = t.base + token;
     u32x4 qf[D / 32];
     {
@@ -375,29 +369,27 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, u
         }
     }
     if (wave != 0 || lq >= t.rows) return;
-    const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, plane = (int64_t)split * b.n_tokens * a.heads + to_row;
-    if (share.parts == 1) {
+    const int64_t to_row = (int64_t)(t.first + token) * a.heads + q_head, place = (t.slot + (int64_t)t.split * c.heads) * ROWS + lq;
+    if (t.parts == 1) {
         const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
         uint16_t *out = (uint16_t *)a.out + (t.first + token) * a.out_stride + q_head * D + g * 4;
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) *(u32x2 *)(out + e * 16) = u32x2{cache_pair<BF>(o[e][0] * inv, o[e][1] * inv), cache_pair<BF>(o[e][2] * inv, o[e][3] * inv)};
     } else {
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) *(float4v *)(partials.sums + plane * D + g * 4 + e * 16) = o[e];
+        for (int e = 0; e < D / 16; ++e) *(float4v *)(partials.sums + place * D + g * 4 + e * 16) = o[e];
     }
-    if (splits > 1 && g == 0) {
-        partials.top_weight[plane * 2] = top;
-        partials.top_weight[plane * 2 + 1] = sum;
-        if (split == 0) partials.parts[to_row] = share.parts;
+    if (cut.slots > 0 && g == 0) {
+        partials.top_weight[place * 2] = top;
+        partials.top_weight[place * 2 + 1] = sum;
+        if (t.split == 0) partials.rows[to_row] = {(int32_t)place, t.parts};
     }
 }
 
 template <int BITS, bool BF, int D>
 void launch_few(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
-    const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    launch(cache_few_kernel<BITS, BF, D, 4>, grid, dim3(256), 0, stream, a, gr, hr, sr, cut.splits, cut.keys, partials);
+    launch(cache_few_kernel<BITS, BF, D, 4>, dim3((uint32_t)cut.blocks), dim3(256), 0, stream, a, cut.work, partials);
 }
 template <bool BF, int D>
 void launch_bits(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)

@@ -26,7 +26,7 @@ __device__ inline float16v product(u32x4 a, u32x4 b, float16v c)
 }
 template <int BITS, int D, int WR, int WK>
 struct TileShape {
-    static constexpr int KT = WR == 4 ? 64 : 32;         // keys of a step
+    static constexpr int KT = WR >= 4 ? 64 : 32;         // keys of a step
     static constexpr int BUFFERS = 2;
     static constexpr int THREADS = 64 * WR;              // of a group
     static constexpr int KS = D + 8, VS = D + 32;        // halves per row in LDS: no two lanes of a read share a bank
@@ -37,12 +37,11 @@ struct TileShape {
     static constexpr int JOIN_FLOATS = WK > 1 ? WK * 32 * WR * (D + 4) : 0;   // results of the groups, at the end
     static constexpr int STAGE_BYTES = STEP_BYTES * BUFFERS * WK;
     static constexpr int LDS_BYTES = STAGE_BYTES > JOIN_FLOATS * 4 ? STAGE_BYTES : JOIN_FLOATS * 4;
-    static_assert(WR * WK == 4 && KT * ROW_CHUNKS % THREADS == 0, "");
+    static_assert(KT * ROW_CHUNKS % THREADS == 0, "");
 };
 
 template <int BITS, bool BF, int D, int WR, int WK>
-__global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, uint32_t group_recip, uint32_t heads_recip, uint32_t splits_recip, int tiles,
-                                                             int splits, int per_split, Partials partials)
+__global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionCall a, WorkCut cut, Partials partials)
 {
     using T = TileShape<BITS, D, WR, WK>;
     constexpr int KT = T::KT, KS = T::KS, VS = T::VS, ROWS = 32 * WR, NKB = KT / 32, ROW_BYTES = D * BITS / 8, CHUNK_BYTES = T::CHUNK * BITS / 8;
@@ -54,21 +53,18 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     const BatchView &b = a.batch;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const int g = lane >> 5, lr = lane & 31, tid = wr * 64 + lane;   // (tid: inside the group)
-    // blocks in the order (tile, split, head), the last tiles first: the heads of a tile, which share nothing, go to different XCDs and the tiles
-    // of a head, which read the same keys, to one or a few; the later a tile of a sequence, the more keys it has
-    const int tile_split = quotient(blockIdx.x, c.heads, heads_recip), head = blockIdx.x - tile_split * c.heads;
-    const int from_last = quotient(tile_split, splits, splits_recip), tile = tiles - 1 - from_last, split = tile_split - from_last * splits;
-    const QueryTile t = find_tile(c, b, tile, a.group, group_recip, ROWS, a.window, a.sinks);
+    // blocks in the order (item, head): the heads of a tile, which share nothing, go to different XCDs and the tiles of a head, which read the
+    // same keys, to one or a few
+    const int from_last = quotient(blockIdx.x, c.heads, cut.heads_recip), head = blockIdx.x - from_last * c.heads;
+    const QueryTile t = find_work(c, b, cut, from_last, head, a.group, a.window, a.sinks);
     if (t.seq < 0) return;
-    const KeyShare share = key_share(t.keys, split, per_split);
-    if (split >= share.parts) return;
 
     // this lane's query as the B operand of S^T = K Q^T
-    const int row = t.row0 + min(wr * 32 + lr, t.rows - 1), token = quotient(row, a.group, group_recip);
+    const int row = t.row0 + min(wr * 32 + lr, t.rows - 1), token = quotient(row, a.group, cut.group_recip);
     const int pos = t.base + token, q_head = head * a.group + row - token * a.group;
     const bool idle = wr * 32 >= t.rows;
     const int wave_last = t.row0 + min(wr * 32 + 31, t.rows - 1);
-    const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, group_recip), last_pos = t.base + quotient(wave_last, a.group, group_recip);
+    const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, cut.group_recip), last_pos = t.base + quotient(wave_last, a.group, cut.group_recip);
     u32x4 qf[D / 16];
     float back = 1.f;   // what the scores of queries brought into binary16's range are multiplied by
     {
@@ -100,9 +96,9 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             for (int s = 0; s < D / 16; ++s) qf[s] = in_nibble_order(qf[s]);
     }
 
-    const int x_end = share.end, steps = (x_end - share.begin + KT - 1) / KT;
+    const int x_end = t.end, steps = (x_end - t.begin + KT - 1) / KT;
     const int rounds = (steps + WK - 1) / WK;   // the same for all groups: they meet at barriers
-    const int x_first = share.begin + wk * KT, x_stride = WK * KT;   // the group's steps
+    const int x_first = t.begin + wk * KT, x_stride = WK * KT;   // the group's steps
 
     float16v o[D / 32];
 #pragma unroll
@@ -197,9 +193,12 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     __syncthreads();
     for (int n = 0; n < rounds; ++n) {
         const int x0 = x_first + n * x_stride, buffer = n & 1;
-        ask_rows(x0 + x_stride);
-        const int pages_next = pages;
-        ask_pages(x0 + 2 * x_stride);
+        const bool more = n + 1 < rounds;
+        int pages_next = pages;
+        if (more) {
+            ask_rows(x0 + x_stride);
+            ask_pages(x0 + 2 * x_stride);
+        }
         const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
         const bool none = idle || x0 >= x_end || key_first > last_pos || (a.window > 0 && key_first >= a.sinks && key_last <= first_pos - a.window);
         auto compute = [&](auto all_see, uint64_t held) {   // all_see: whether every query of the wave sees every key of the step
@@ -317,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             else
                 compute(std::false_type(), held);
         }
-        put_rows((n + 1) & 1, n + 1, pages_next);
+        if (more) put_rows((n + 1) & 1, n + 1, pages_next);
         __syncthreads();
         pages_now = pages_next;
     }
@@ -340,12 +339,12 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
     }
     sum = pair_sum(across_32(sum));
     if constexpr (BITS == 16) top = top == -INFINITY ? top : top * a.scale;
-    const int64_t plane = (int64_t)split * b.n_tokens * a.heads;
+    const int64_t place0 = (t.slot + (int64_t)t.split * c.heads) * ROWS;
     if constexpr (WK == 1) {
         if (wr * 32 + lr >= t.rows) return;
         const int64_t to_row = (int64_t)(t.first + token);
-        const int64_t in_plane = to_row * a.heads + q_head, at = plane + in_plane;
-        if (share.parts == 1) {
+        const int64_t place = place0 + wr * 32 + lr;
+        if (t.parts == 1) {
             const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
             uint16_t *out = (uint16_t *)a.out + to_row * a.out_stride + q_head * D + g * 4;
 #pragma unroll
@@ -356,16 +355,16 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
                     *(u32x2 *)(out + e * 32 + v4 * 8) = w;
                 }
         } else {
-            float *out = partials.sums + at * D + g * 4;
+            float *out = partials.sums + place * D + g * 4;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e)
 #pragma unroll
                 for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(out + e * 32 + v4 * 8) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
         }
-        if (splits > 1 && g == 0) {
-            partials.top_weight[at * 2] = top;
-            partials.top_weight[at * 2 + 1] = sum;
-            if (split == 0) partials.parts[in_plane] = share.parts;
+        if (cut.slots > 0 && g == 0) {
+            partials.top_weight[place * 2] = top;
+            partials.top_weight[place * 2 + 1] = sum;
+            if (t.split == 0) partials.rows[to_row * a.heads + q_head] = {(int32_t)place, t.parts};
         }
     } else {
         // the groups' results, over the staged steps
@@ -382,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
             weights[wk][wr * 32 + lr] = sum;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < t.rows * (D / 4); i += 256) {
+        for (int i = threadIdx.x; i < t.rows * (D / 4); i += 64 * WR * WK) {
             const int r = i / (D / 4), at = i % (D / 4) * 4;
             float m = tops[0][r], l = 0.f;
 #pragma unroll
@@ -396,19 +395,19 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] += x[j] * f;
             }
-            const int rr = t.row0 + r, tok = quotient(rr, a.group, group_recip), qh = head * a.group + rr - tok * a.group;
-            const int64_t in_plane = (int64_t)(t.first + tok) * a.heads + qh, to = plane + in_plane;
-            if (share.parts == 1) {
+            const int rr = t.row0 + r, tok = quotient(rr, a.group, cut.group_recip), qh = head * a.group + rr - tok * a.group;
+            const int64_t place = place0 + r;
+            if (t.parts == 1) {
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
                 const u32x2 w = {cache_pair<BF>(v[0] * inv, v[1] * inv), cache_pair<BF>(v[2] * inv, v[3] * inv)};
                 *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + at) = w;
             } else {
-                *(float4v *)(partials.sums + to * D + at) = v;
+                *(float4v *)(partials.sums + place * D + at) = v;
             }
-            if (splits > 1 && at == 0) {
-                partials.top_weight[to * 2] = m;
-                partials.top_weight[to * 2 + 1] = l;
-                if (split == 0) partials.parts[in_plane] = share.parts;
+            if (cut.slots > 0 && at == 0) {
+                partials.top_weight[place * 2] = m;
+                partials.top_weight[place * 2 + 1] = l;
+                if (t.split == 0) partials.rows[(int64_t)(t.first + tok) * a.heads + qh] = {(int32_t)place, t.parts};
             }
         }
     }
@@ -417,13 +416,11 @@ __global__ __launch_bounds__(256, 2) void cache_tiles_kernel(AttentionCall a, ui
 template <int BITS, bool BF, int D>
 void launch_tiles(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(cut.tiles * cut.splits * a.cache.heads));
-    const uint32_t gr = reciprocal((uint32_t)a.group), hr = reciprocal((uint32_t)a.cache.heads), sr = reciprocal((uint32_t)cut.splits);
-    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, gr, hr, sr, (int)cut.tiles, cut.splits, cut.keys, partials); };
-    if (cut.tile_rows == 64)
-        go(cache_tiles_kernel<BITS, BF, D, 2, 2>);
+    auto go = [&](auto kernel, int threads) { launch(kernel, dim3((uint32_t)cut.blocks), dim3(threads), 0, stream, a, cut.work, partials); };
+    if (cut.work.rows == 64)
+        go(cache_tiles_kernel<BITS, BF, D, 2, 2>, 256);
     else
-        go(cache_tiles_kernel<BITS, BF, D, 4, 1>);
+        go(cache_tiles_kernel<BITS, BF, D, 4, 1>, 256);
 }
 template <bool BF, int D>
 void launch_bits(const AttentionCall &a, const AttentionCut &cut, const Partials &partials, hipStream_t stream)
