@@ -133,10 +133,10 @@ __global__ __launch_bounds__(kWaves * 64) void cache_attention_kernel(AttentionC
         for (int u = 0; u < U; ++u) {
             const int x = x0 + u * AT_ONCE + group_lane;
             key[u] = t.keys.key(min(x, x_end - 1));
-            const int page = cache_page(c, b, t.seq, key[u]);
-            there[u] = x < x_end && page >= 0;
-            plain &= page >= 0;
-            const int64_t row = (int64_t)cache_row(c, max(page, 0), head, key[u]);
+            const int page = cache_page(b, c, t.seq, key[u]);
+            there[u] = x < x_end && is_page(c, page);
+            plain &= is_page(c, page);
+            const int64_t row = (int64_t)cache_row(c, page_or_0(c, page), head, key[u]);
             k[u].load(c.k + row * ROW_BYTES + part * P::BYTES);
             v[u].load(c.v + row * ROW_BYTES + part * P::BYTES);
             if constexpr (BITS < 16) {

@@ -71,14 +71,14 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, W
     uint32_t row = 0;
     uint64_t held = 0;
     auto key_of = [&](int x) { return t.keys.key(min(x + (lane & (KT - 1)), x_end - 1)); };
-    auto ask_pages = [&](int x) { page = cache_page(c, b, t.seq, key_of(x)); };
+    auto ask_pages = [&](int x) { page = cache_page(b, c, t.seq, key_of(x)); };
     u32x4 kr[NKB][KP], vr[VP];
     auto v_row = [&](int i) { return (i * 64 + lane) / (T::ROW / PIECE); };              // key and byte of the lane's piece i of a step's values
     auto v_at = [&](int i) { return (i * 64 + lane) % (T::ROW / PIECE) * PIECE; };
     float scale = 0.f, scale_v = 0.f;
     auto ask_rows = [&](int x) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
-        held = __ballot(page >= 0);
-        row = cache_row(c, max(page, 0), head, key_of(x));
+        held = __ballot(is_page(c, page));
+        row = cache_row(c, page_or_0(c, page), head, key_of(x));
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
             // key of this lane's row of block kb: each group of lanes ends up with consecutive keys in its registers of S^T
@@ -162,6 +162,9 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, W
         ask_rows(x0);
         ask_pages(x0 + x_stride);
     }
+    // the queries are there before the loop: or each step would wait for every request in front of its first use of them
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(qf[i]));
     // (one way through a step, branches around what few steps need: registers that two ways leave in different places are copied, and requests on
     // their way waited for)
     for (; x0 < x_end; x0 += x_stride) {

@@ -113,10 +113,10 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
     int pages = -1, pages_now = -1;   // of key `lane` % KT of a step
     auto ask_pages = [&](int x0) {
         const int x = x0 + (lane & (KT - 1));
-        pages = cache_page(c, b, t.seq, t.keys.key(min(x, x_end - 1)));
+        pages = cache_page(b, c, t.seq, t.keys.key(min(x, x_end - 1)));
     };
     auto ask_rows = [&](int x0) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
-        const uint32_t of_key = cache_row(c, max(pages, 0), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));   // row of key `lane` % KT
+        const uint32_t of_key = cache_row(c, page_or_0(c, pages), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));   // row of key `lane` % KT
 #pragma unroll
         for (int i = 0; i < T::ITEMS; ++i) {
             const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, part = item % T::ROW_CHUNKS;
@@ -136,19 +136,22 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
         }
     };
     auto step_lds = [&](int buffer) { return lds + (wk * T::BUFFERS + buffer) * T::STEP_BYTES; };
+    // whether every query of the tile sees every key of a step (the same for all waves of a group)
+    auto seen_by_all = [&](int x0, int of_pages) {
+        const int key_first = t.keys.key(x0), key_last = t.keys.key(x0 + KT - 1);
+        return x0 + KT <= x_end && key_last <= t.first_pos && (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks) &&
+               __all(is_page(c, of_pages));
+    };
     auto put_rows = [&](int buffer, int n, int of_pages) {   // n: the step's number inside the group
-        if (BITS == 16) {
-            const int x0 = x_first + n * x_stride;
-            const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
-            const bool seen_by_all = x0 + KT <= x_end && key_last <= t.first_pos && (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks);
-            if (!seen_by_all || __any(of_pages < 0)) {
-                uint32_t odd = 0;
+        if (BITS == 16 && !seen_by_all(x_first + n * x_stride, of_pages)) {
+            uint32_t odd = 0;
 #pragma unroll
-                for (int i = 0; i < T::ITEMS; ++i)
+            for (int i = 0; i < T::ITEMS; ++i) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) odd |= odd_halves<BF>(vr[i][j]);
-                if (odd) odd_step[wk][buffer] = n;
+                for (int j = 0; j < 4; ++j) odd |= odd_halves<BF>(vr[i][j]);
+                vr[i] = without_odd<BF>(vr[i]);
             }
+            if (odd) odd_step[wk][buffer] = n;
         }
         uint16_t *ks = (uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
 #pragma unroll
@@ -191,18 +194,23 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
         put_rows(0, 0, pages_now);
     }
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));   // there before the loop: or each step would wait for every request in front of them
+    // (one way through a step, branches around what few steps need: registers that two ways leave in different places are copied)
     for (int n = 0; n < rounds; ++n) {
         const int x0 = x_first + n * x_stride, buffer = n & 1;
         const bool more = n + 1 < rounds;
-        int pages_next = pages;
+        const int pages_next = pages;
         if (more) {
             ask_rows(x0 + x_stride);
             ask_pages(x0 + 2 * x_stride);
         }
         const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
         const bool none = idle || x0 >= x_end || key_first > last_pos || (a.window > 0 && key_first >= a.sinks && key_last <= first_pos - a.window);
-        auto compute = [&](auto all_see, uint64_t held) {   // all_see: whether every query of the wave sees every key of the step
-            constexpr bool PLAIN = decltype(all_see)::value;
+        if (!none) {
+            const uint64_t held = __ballot(is_page(c, pages_now));   // bit j: the page of key j is there (KT 32: bits twice)
+            const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
+                               (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);   // the wave's queries see all keys
             const uint16_t *ks = (const uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
             const float *sc = (const float *)(vs + KT * VS);
             float16v s[NKB];
@@ -224,14 +232,35 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
                         for (int v = 0; v < 4; ++v) s[kb][v4 * 4 + v] = fmaf(BF ? s[kb][v4 * 4 + v] * back : s[kb][v4 * 4 + v], k4[v], l4[v]);
                     }
             }
-            uint64_t seen = 0;
-            if constexpr (!PLAIN) {
-                seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held;
+            if (!plain) {
+                const uint64_t seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held;
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb) {
                     const uint32_t mine = (uint32_t)(seen >> (kb * 32)) >> (g * 4);
 #pragma unroll
                     for (int v = 0; v < 16; ++v) s[kb][v] = mine & (1u << ((v >> 2) * 8 + (v & 3))) ? s[kb][v] : -INFINITY;
+                }
+            }
+            if (BITS == 16 && !seen_by_all(x0, pages_now) && uniform(odd_step[wk][buffer]) == n) {
+                // values that are not finite, which put_rows has kept from the products: from memory to the queries that see them
+                const uint64_t seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held;
+#pragma unroll 1
+                for (int j = 0; j < KT; ++j) {
+                    const bool see = seen >> j & 1;
+                    const int page = __shfl(pages_now, j & (KT - 1));
+                    const uint64_t row_at = (uint64_t)cache_row(c, page_or_0(c, page), head, t.keys.key(min(x0 + j, x_end - 1))) * ROW_BYTES;
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+                        for (int v4 = 0; v4 < 4; ++v4) {
+                            const u32x2 w = *(const u32x2 *)(c.v + row_at + (e * 32 + v4 * 8 + g * 4) * 2);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
+                                if (bad & 1) o[e][v4 * 4 + 2 * i] += cache_number<BF>(pair & 0xFFFFu);
+                                if (bad >> 31) o[e][v4 * 4 + 2 * i + 1] += cache_number<BF>(pair >> 16);
+                            }
+                        }
                 }
             }
             float m = s[0][0];
@@ -251,25 +280,6 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
                 for (int e = 0; e < D / 32; ++e)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) o[e][v] *= f;
-            }
-            const bool odd = BITS == 16 && !PLAIN && uniform(odd_step[wk][buffer]) == n;
-            if (odd) {
-#pragma unroll 1
-                for (int j = 0; j < KT; ++j) {
-                    const bool see = seen >> j & 1;
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-                        for (int v4 = 0; v4 < 4; ++v4) {
-                            const u32x2 w = *(const u32x2 *)(vs + j * VS + e * 32 + v4 * 8 + g * 4);
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint32_t pair = w[i], bad = see ? odd_halves<BF>(pair) : 0u;
-                                if (bad & 1) o[e][v4 * 4 + 2 * i] += cache_number<BF>(pair & 0xFFFFu);
-                                if (bad >> 31) o[e][v4 * 4 + 2 * i + 1] += cache_number<BF>(pair >> 16);
-                            }
-                        }
-                }
             }
             const float shift = top == -INFINITY ? 0.f : -top * scale;
 #pragma unroll
@@ -300,21 +310,10 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
                         typedef __attribute__((address_space(3))) short4v *LdsShort4;
                         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + e * 32)));
                         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(vrow + 8 * VS + e * 32)));
-                        u32x4 vf = {lo.x, lo.y, hi.x, hi.y};
-                        if (BITS == 16 && !PLAIN && odd) vf = without_odd<BF>(vf);
-                        o[e] = product<MBF>(vf, pf, o[e]);
+                        o[e] = product<MBF>(u32x4{lo.x, lo.y, hi.x, hi.y}, pf, o[e]);
                     }
                 }
             }
-        };
-        if (!none) {
-            const uint64_t held = __ballot(pages_now >= 0);   // bit j: the page of key j is there (KT 32: bits twice)
-            const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
-                               (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);
-            if (plain)
-                compute(std::true_type(), held);
-            else
-                compute(std::false_type(), held);
         }
         if (more) put_rows((n + 1) & 1, n + 1, pages_next);
         __syncthreads();

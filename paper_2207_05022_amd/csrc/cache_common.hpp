@@ -27,12 +27,14 @@ __device__ inline uint32_t cache_row(const CacheView &c, int page, int head, int
 {
     return (((uint32_t)page * c.heads + head) << c.page_shift) + (position & ((1 << c.page_shift) - 1));
 }
-// Page of a position (0 <= position < capacity), or -1 where the table names none of the pool's.
-__device__ inline int cache_page(const CacheView &c, const BatchView &b, int seq, int position)
+// Entry of the table for a position (0 <= position < capacity), and whether it names one of the pool's pages.  (Apart: what is asked for ahead is
+// looked at where it is used, or the request is waited for where it is made.)
+__device__ inline int cache_page(const BatchView &b, const CacheView &c, int seq, int position)
 {
-    const int page = b.table[(int64_t)seq * b.max_pages + (position >> c.page_shift)];
-    return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
+    return b.table[(int64_t)seq * b.max_pages + (position >> c.page_shift)];
 }
+__device__ inline bool is_page(const CacheView &c, int page) { return (uint32_t)page < (uint32_t)c.n_pages; }
+__device__ inline int page_or_0(const CacheView &c, int page) { return is_page(c, page) ? page : 0; }
 __device__ inline int cache_capacity(const CacheView &c, const BatchView &b) { return b.max_pages << c.page_shift; }
 
 // A sequence's new rows and its length, inside what the structs promise whatever the caller's arrays hold.  Positions, lengths and windows stay

@@ -166,8 +166,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
     load8<IO>(v, token * v_stride + head * D + part * 8, xv);
     int seq, position;
     find_slot<LANES>(c, b, token, &seq, &position);
-    const int page = seq >= 0 && row_in <= last ? cache_page(c, b, seq, position) : -1;
-    if (page < 0) return;   // (whole groups of lanes)
+    const int page = seq >= 0 && row_in <= last ? cache_page(b, c, seq, position) : -1;
+    if (!is_page(c, page)) return;   // (whole groups of lanes)
     const int64_t at = cache_row(c, page, head, position);
     store_row<BITS, STORED, D>((void *)c.k, (float *)c.k_scale, at, part, xk);
     store_row<BITS, STORED, D>((void *)c.v, (float *)c.v_scale, at, part, xv);
@@ -208,9 +208,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
     if (seq >= b.n_seqs || j >= count) return;
     const int position = first + j;
     int page = -1;
-    if (position < min(b.lengths[seq], cache_capacity(c, b))) page = cache_page(c, b, seq, position);
+    if (position < min(b.lengths[seq], cache_capacity(c, b))) page = cache_page(b, c, seq, position);
     float xk[8] = {}, xv[8] = {};
-    if (page >= 0) {
+    if (is_page(c, page)) {
         const int64_t at = cache_row(c, page, head, position);
         load_row<BITS, STORED, D>(c.k, c.k_scale, at, part, xk);
         load_row<BITS, STORED, D>(c.v, c.v_scale, at, part, xv);
