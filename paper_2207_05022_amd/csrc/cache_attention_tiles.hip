@@ -28,6 +28,7 @@ template <int BITS, int D, int WR, int WK>
 struct TileShape {
     static constexpr int KT = WR >= 4 ? 64 : 32;         // keys of a step
     static constexpr int BUFFERS = 2;
+    static constexpr int AHEAD = BITS == 16 && D == 128 ? 1 : 2;   // steps whose rows are in registers (16-bit rows of 128 values: no room for two)
     static constexpr int THREADS = 64 * WR;              // of a group
     static constexpr int KS = D + 8, VS = D + 32;        // halves per row in LDS: no two lanes of a read share a bank
     static constexpr int CHUNK = BITS == 16 ? 8 : 16;    // values of a request: 16 bytes, 8 of codes of 4 bits
@@ -107,49 +108,53 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
         for (int v = 0; v < 16; ++v) o[e][v] = 0.f;
     float top = -INFINITY, sum = 0.f;   // (16 bits: top in units of the unscaled scores; sum: of this lane's keys)
 
-    // one step on its way: raw rows in registers, pages of the one behind it
-    u32x4 kr[T::ITEMS], vr[T::ITEMS];
-    float scale_k = 0.f, scale_v = 0.f;
-    int pages = -1, pages_now = -1;   // of key `lane` % KT of a step
-    auto ask_pages = [&](int x0) {
-        const int x = x0 + (lane & (KT - 1));
-        pages = cache_page(b, c, t.seq, t.keys.key(min(x, x_end - 1)));
+    // Steps on their way: their rows as stored, in registers, AHEAD steps in front of the products (one: what a step's products take is less than
+    // the way to memory), and the page entries of the step behind them, asked for in front of the rows so that waiting for them waits for no row.
+    struct Rows {
+        u32x4 k[T::ITEMS], v[T::ITEMS];
+        float scale_k, scale_v;   // of key `lane` % KT
+        uint64_t held;            // bit j: the page of key j is there (KT 32: bits twice)
     };
-    auto ask_rows = [&](int x0) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
+    int pages = -1;   // of key `lane` % KT of the step behind the last one asked for
+    auto ask_pages = [&](int x0) { pages = cache_page(b, c, t.seq, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1))); };
+    auto ask = [&](Rows &rows, int x0) {   // (behind the share's end: its last row again; a branch would hold the registers of both ways)
+        rows.held = __ballot(is_page(c, pages));
         const uint32_t of_key = cache_row(c, page_or_0(c, pages), head, t.keys.key(min(x0 + (lane & (KT - 1)), x_end - 1)));   // row of key `lane` % KT
+        ask_pages(x0 + x_stride);
 #pragma unroll
         for (int i = 0; i < T::ITEMS; ++i) {
             const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, part = item % T::ROW_CHUNKS;
             const uint64_t at = (uint64_t)(uint32_t)__shfl((int)of_key, r) * ROW_BYTES + part * CHUNK_BYTES;
             if constexpr (BITS == 4) {
                 const u32x2 k2 = *(const u32x2 *)(c.k + at), v2 = *(const u32x2 *)(c.v + at);
-                kr[i] = u32x4{k2.x, k2.y, 0, 0};
-                vr[i] = u32x4{v2.x, v2.y, 0, 0};
+                rows.k[i] = u32x4{k2.x, k2.y, 0, 0};
+                rows.v[i] = u32x4{v2.x, v2.y, 0, 0};
             } else {
-                kr[i] = *(const u32x4 *)(c.k + at);
-                vr[i] = *(const u32x4 *)(c.v + at);
+                rows.k[i] = *(const u32x4 *)(c.k + at);
+                rows.v[i] = *(const u32x4 *)(c.v + at);
             }
         }
         if constexpr (BITS < 16) {
-            scale_k = c.k_scale[of_key];
-            scale_v = c.v_scale[of_key];
+            rows.scale_k = c.k_scale[of_key];
+            rows.scale_v = c.v_scale[of_key];
         }
     };
     auto step_lds = [&](int buffer) { return lds + (wk * T::BUFFERS + buffer) * T::STEP_BYTES; };
     // whether every query of the tile sees every key of a step (the same for all waves of a group)
-    auto seen_by_all = [&](int x0, int of_pages) {
+    auto seen_by_all = [&](int x0, uint64_t held) {
         const int key_first = t.keys.key(x0), key_last = t.keys.key(x0 + KT - 1);
         return x0 + KT <= x_end && key_last <= t.first_pos && (a.window <= 0 || key_first > t.last_pos - a.window || key_last < a.sinks) &&
-               __all(is_page(c, of_pages));
+               held == ~(uint64_t)0;
     };
-    auto put_rows = [&](int buffer, int n, int of_pages) {   // n: the step's number inside the group
-        if (BITS == 16 && !seen_by_all(x_first + n * x_stride, of_pages)) {
+    auto put_rows = [&](Rows &rows, int n) {   // n: the step's number inside the group
+        const int buffer = n & 1;
+        if (BITS == 16 && !seen_by_all(x_first + n * x_stride, rows.held)) {
             uint32_t odd = 0;
 #pragma unroll
             for (int i = 0; i < T::ITEMS; ++i) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) odd |= odd_halves<BF>(vr[i][j]);
-                vr[i] = without_odd<BF>(vr[i]);
+                for (int j = 0; j < 4; ++j) odd |= odd_halves<BF>(rows.v[i][j]);
+                rows.v[i] = without_odd<BF>(rows.v[i]);
             }
             if (odd) odd_step[wk][buffer] = n;
         }
@@ -159,25 +164,25 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
             const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, at = item % T::ROW_CHUNKS * T::CHUNK;
             u32x4 *kd = (u32x4 *)(ks + r * KS + at), *vd = (u32x4 *)(vs + r * VS + at);
             if constexpr (BITS == 16) {
-                kd[0] = kr[i];
-                vd[0] = vr[i];
+                kd[0] = rows.k[i];
+                vd[0] = rows.v[i];
             } else if constexpr (BITS == 8) {
-                kd[0] = numbers_of_bytes(kr[i][0], kr[i][1]);
-                kd[1] = numbers_of_bytes(kr[i][2], kr[i][3]);
-                vd[0] = numbers_of_bytes(vr[i][0], vr[i][1]);
-                vd[1] = numbers_of_bytes(vr[i][2], vr[i][3]);
+                kd[0] = numbers_of_bytes(rows.k[i][0], rows.k[i][1]);
+                kd[1] = numbers_of_bytes(rows.k[i][2], rows.k[i][3]);
+                vd[0] = numbers_of_bytes(rows.v[i][0], rows.v[i][1]);
+                vd[1] = numbers_of_bytes(rows.v[i][2], rows.v[i][3]);
             } else {
-                kd[0] = numbers_of_nibbles(kr[i][0]);
-                kd[1] = numbers_of_nibbles(kr[i][1]);
-                vd[0] = numbers_of_nibbles(vr[i][0]);
-                vd[1] = numbers_of_nibbles(vr[i][1]);
+                kd[0] = numbers_of_nibbles(rows.k[i][0]);
+                kd[1] = numbers_of_nibbles(rows.k[i][1]);
+                vd[0] = numbers_of_nibbles(rows.v[i][0]);
+                vd[1] = numbers_of_nibbles(rows.v[i][1]);
             }
         }
         if constexpr (BITS < 16) {
             float *sc = (float *)(vs + KT * VS);
             if (tid < KT) {
-                const ValueScale s = value_scale(scale_v);
-                sc[tid] = scale_k * a.scale;
+                const ValueScale s = value_scale(rows.scale_v);
+                sc[tid] = rows.scale_k * a.scale;
                 sc[KT + tid] = s.log;
                 sc[2 * KT + tid] = s.inverse;
             }
@@ -186,29 +191,28 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
     if (lane == 0)
         for (int i = 0; i < T::BUFFERS; ++i) odd_step[wk][i] = -1;   // (the waves of a group write the same; a find comes behind the barrier)
     __syncthreads();
+    Rows rows[T::AHEAD];
+    uint64_t held = 0, held_next = 0;   // of the step at hand, and the next one
     if (rounds > 0) {
         ask_pages(x_first);
-        ask_rows(x_first);
-        pages_now = pages;
-        ask_pages(x_first + x_stride);
-        put_rows(0, 0, pages_now);
+        ask(rows[0], x_first);
+        if constexpr (T::AHEAD == 2) {
+            ask(rows[1], x_first + x_stride);
+            held_next = rows[1].held;
+        }
+        held = rows[0].held;
+        put_rows(rows[0], 0);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));   // there before the loop: or each step would wait for every request in front of them
     // (one way through a step, branches around what few steps need: registers that two ways leave in different places are copied)
-    for (int n = 0; n < rounds; ++n) {
+    auto step = [&](int n, Rows &asked, Rows &next) {   // asked: of the step AHEAD behind this one; next: of the next
         const int x0 = x_first + n * x_stride, buffer = n & 1;
-        const bool more = n + 1 < rounds;
-        const int pages_next = pages;
-        if (more) {
-            ask_rows(x0 + x_stride);
-            ask_pages(x0 + 2 * x_stride);
-        }
+        if (n + T::AHEAD < rounds) ask(asked, x0 + T::AHEAD * x_stride);
         const int key_first = t.keys.key(x0), key_last = t.keys.key(min(x0 + KT, x_end) - 1);
         const bool none = idle || x0 >= x_end || key_first > last_pos || (a.window > 0 && key_first >= a.sinks && key_last <= first_pos - a.window);
         if (!none) {
-            const uint64_t held = __ballot(is_page(c, pages_now));   // bit j: the page of key j is there (KT 32: bits twice)
             const bool plain = x0 + KT <= x_end && held == ~(uint64_t)0 && key_last <= first_pos &&
                                (a.window <= 0 || key_first > last_pos - a.window || key_last < a.sinks);   // the wave's queries see all keys
             const uint16_t *ks = (const uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
@@ -241,14 +245,14 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
                     for (int v = 0; v < 16; ++v) s[kb][v] = mine & (1u << ((v >> 2) * 8 + (v & 3))) ? s[kb][v] : -INFINITY;
                 }
             }
-            if (BITS == 16 && !seen_by_all(x0, pages_now) && uniform(odd_step[wk][buffer]) == n) {
+            if (BITS == 16 && !seen_by_all(x0, held) && uniform(odd_step[wk][buffer]) == n) {
                 // values that are not finite, which put_rows has kept from the products: from memory to the queries that see them
                 const uint64_t seen = seen_keys(t.keys, pos, a.window, a.sinks, x0, x_end) & held;
 #pragma unroll 1
                 for (int j = 0; j < KT; ++j) {
                     const bool see = seen >> j & 1;
-                    const int page = __shfl(pages_now, j & (KT - 1));
-                    const uint64_t row_at = (uint64_t)cache_row(c, page_or_0(c, page), head, t.keys.key(min(x0 + j, x_end - 1))) * ROW_BYTES;
+                    const int key = t.keys.key(min(x0 + j, x_end - 1)), page = cache_page(b, c, t.seq, key);
+                    const uint64_t row_at = (uint64_t)cache_row(c, page_or_0(c, page), head, key) * ROW_BYTES;
 #pragma unroll
                     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -315,9 +319,14 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
                 }
             }
         }
-        if (more) put_rows((n + 1) & 1, n + 1, pages_next);
+        if (n + 1 < rounds) put_rows(next, n + 1);
+        held = T::AHEAD == 2 ? held_next : next.held;
+        held_next = asked.held;
         __syncthreads();
-        pages_now = pages_next;
+    };
+    for (int n = 0; n < rounds; n += T::AHEAD) {
+        step(n, rows[0], rows[T::AHEAD - 1]);
+        if (T::AHEAD == 2 && n + 1 < rounds) step(n + 1, rows[T::AHEAD - 1], rows[0]);
     }
 
     if constexpr (BITS == 4) {
