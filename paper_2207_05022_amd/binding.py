@@ -606,14 +606,16 @@ class StiCacheBatch:
         self.ref = C.byref(self.struct)
 
 
-def _row_stride(t, batch, heads: int, d_head: int, name: str) -> int:
+def _row_stride(t, n_tokens: int, heads: int, d_head: int, name: str) -> int:
     """Stride between the rows of t [n_tokens, heads, d_head], whose rows lie as one piece each."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[1] != heads or shape[2] != d_head:
-        raise ValueError(f"{name} must be [{batch.n_tokens}, {heads}, {d_head}], not {list(shape)}")
-    if (strides[2] != 1 and d_head > 1) or (strides[1] != d_head and heads > 1):
+    if t.shape != (n_tokens, heads, d_head):
+        raise ValueError(f"{name} must be [{n_tokens}, {heads}, {d_head}], not {list(t.shape)}")
+    if t.is_contiguous():
+        return heads * d_head
+    strides = t.stride()
+    if strides[2] != 1 or (strides[1] != d_head and heads > 1):
         raise ValueError(f"the values of a row of {name} must lie behind each other")
-    return strides[0] if shape[0] > 1 else heads * d_head
+    return strides[0] if n_tokens > 1 else heads * d_head
 
 
 def sti_cache_append(cache: StiCache, batch: StiCacheBatch, k, v, stream=None) -> None:
@@ -622,7 +624,7 @@ def sti_cache_append(cache: StiCache, batch: StiCacheBatch, k, v, stream=None) -
         raise ValueError("k and v must have one dtype")
     heads, d = cache.n_kv_heads, cache.d_head
     st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k),
-                              _row_stride(k, batch, heads, d, "k"), _row_stride(v, batch, heads, d, "v"), _stream_handle(stream))
+                              _row_stride(k, batch.n_tokens, heads, d, "k"), _row_stride(v, batch.n_tokens, heads, d, "v"), _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_cache_append")
 
@@ -651,8 +653,8 @@ def sti_cache_attention(cache: StiCache, batch: StiCacheBatch, q, out, workspace
     if q.dtype != out.dtype:
         raise ValueError("q and out must have one dtype")
     heads, d = q.shape[1], cache.d_head
-    st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), _row_stride(q, batch, heads, d, "q"),
-                                 _row_stride(out, batch, heads, d, "out"), heads, scale, window, sinks, _ptr(workspace),
+    st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), _row_stride(q, batch.n_tokens, heads, d, "q"),
+                                 _row_stride(out, batch.n_tokens, heads, d, "out"), heads, scale, window, sinks, _ptr(workspace),
                                  _nbytes(workspace), _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_cache_attention")

@@ -78,7 +78,7 @@ bool valid_heads(const sti_cache &c, const sti_cache_batch &b, int32_t n_heads)
 
 AttentionCut cut_of(const sti_cache &c, const sti_cache_batch &b, int32_t n_heads, int32_t window, int32_t sinks)
 {
-    return attention_cut(b.n_tokens, b.n_seqs, n_heads, c.n_kv_heads, (int64_t)b.max_pages * c.page_tokens, window, sinks);
+    return attention_cut(b.n_tokens, b.n_seqs, n_heads, c.n_kv_heads, c.d_head, (int64_t)b.max_pages * c.page_tokens, window, sinks);
 }
 
 }  // namespace
@@ -111,7 +111,7 @@ sti_status sti_cache_read(const sti_cache *cache, const sti_cache_batch *batch, 
     if (st != STI_OK) return st;
     if (first < 0 || count < 0 || (int64_t)first + count > kMostPositions) return STI_ERR_DIMS;
     if (!known(out_dtype)) return STI_ERR_DTYPE;
-    if (((int64_t)count + 15) / 16 * 16 * batch->n_seqs * cache->n_kv_heads / 16 > kMostBlocks) return STI_ERR_DIMS;
+    if (((int64_t)count + 15) / 16 * 16 * cache->n_kv_heads > kMostBlocks) return STI_ERR_DIMS;   // (rows of a sequence are counted in 32 bits)
     if (batch->n_seqs == 0 || count == 0) return STI_OK;
     st = check_arrays(*cache, *batch, false);
     if (st != STI_OK) return st;

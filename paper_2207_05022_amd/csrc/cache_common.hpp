@@ -185,12 +185,6 @@ __device__ inline QueryTile find_work(const CacheView &c, const BatchView &b, co
     return t;
 }
 
-// Whether a query at `pos` sees `key` (a key below its sequence's length).
-__device__ inline bool sees(int pos, int key, int window, int sinks)
-{
-    return key <= pos && (window <= 0 || key > pos - window || key < sinks);
-}
-
 // Bit j of the result: the query at `pos` sees number x0 + j of its tile's keys (below x_end).  Keys grow with their numbers, so that what a query
 // sees is the numbers below `sinks` and those from the window's first to its own.
 __device__ inline uint64_t bits_below(int n) { return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1; }
@@ -224,7 +218,7 @@ struct AttentionCut {
     WorkCut work;
     int64_t blocks;
 };
-AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads, int64_t capacity, int window, int sinks);
+AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads, int d, int64_t capacity, int window, int sinks);
 
 // Partial results where tiles may have several shares, a place for `rows` of them for each work item of each key/value head: sums [place][d], maxima
 // and weights' sums [place][2]; and for each row of the call the place of its first share's and how many shares there are.
