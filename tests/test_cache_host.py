@@ -4,7 +4,16 @@ import math
 
 import pytest
 
-import paper_2207_05022_amd as P
+P = None   # the package, loaded by the first test: a library loaded before torch would bring another HIP runtime into runs of the GPU tests
+
+
+@pytest.fixture(scope="module", autouse=True)
+def load():
+    global P
+    import torch  # noqa: F401
+    import paper_2207_05022_amd
+    P = paper_2207_05022_amd
+
 
 FAKE = 0x10000   # aligned, never dereferenced
 
