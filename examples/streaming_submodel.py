@@ -1,0 +1,120 @@
+"""Tokens streamed through a submodel of shards: causal layers over a paged key/value cache.
+
+The layers are those of sti_layer_forward with causal attention over everything streamed before.  A layer's shards are decoded once
+(sti_decode_shards); each call projects the new tokens, appends their keys and values to the layer's cache (sti_cache_append, straight from
+columns of the projection's output) and lets the new queries read it (sti_cache_attention).
+
+    python examples/streaming_submodel.py          # on an MI355X: chunks and single tokens against one call, caches of 16, 8 and 4 bits
+"""
+from __future__ import annotations
+
+import math
+import os
+import sys
+
+import torch
+import torch.nn.functional as F
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."))
+
+import paper_2207_05022_amd as sti  # noqa: E402
+
+
+class StreamingSubmodel:
+    """`shards[l][i]`: shard objects on the GPU (None = absent); `params[l]`: float32 tensors; a cache of `bits` for `n_seqs` sequences of up to
+    `capacity` tokens per layer.  window, sinks: as in sti_cache_attention."""
+
+    def __init__(self, dims, shards, params, n_seqs, capacity, bits=16, page_tokens=16, window=0, sinks=0):
+        self.dims, self.params, self.window, self.sinks, self.n_seqs = dims, params, window, sinks, n_seqs
+        d, dh, f = dims.d_model, dims.d_head, dims.ffn_per_shard
+        self.layers, self.caches = [], []
+        pages = -(-capacity // page_tokens)
+        for row, p in zip(shards, params):
+            present = [i for i, s in enumerate(row) if s is not None]
+            flat = torch.empty(len(present), dims.weights_per_shard, dtype=torch.float16, device="cuda")
+            sti.sti_decode_shards([row[i] for i in present], dims.weights_per_shard, flat)
+            parts = torch.split(flat, [dh * d, dh * d, dh * d, d * dh, f * d, d * f], dim=1)
+            qkv = torch.cat([w.reshape(-1, d) for w in parts[:3]])                                    # rows: q, k, v of all heads in turn
+            bias = torch.cat([b.reshape(-1, dh)[present].reshape(-1) for b in (p.bq, p.bk, p.bv)]).half()
+            out = parts[3].reshape(-1, d, dh).permute(1, 0, 2).reshape(d, -1).contiguous()
+            up, b1 = parts[4].reshape(-1, d), p.b1.reshape(-1, f)[present].reshape(-1).half()
+            down = parts[5].reshape(-1, d, f).permute(1, 0, 2).reshape(d, -1).contiguous()
+            self.layers.append((len(present), qkv, bias, out, up, b1, down))
+            shape = (n_seqs * pages, len(present), page_tokens)
+            if bits == 16:
+                k, v, scales = torch.zeros(*shape, dh, dtype=torch.float16, device="cuda"), torch.zeros(*shape, dh, dtype=torch.float16, device="cuda"), ()
+            else:
+                held = dict(dtype=torch.int8 if bits == 8 else torch.uint8, device="cuda")
+                k, v = (torch.zeros(*shape, dh * bits // 8, **held) for _ in range(2))
+                scales = tuple(torch.zeros(*shape, device="cuda") for _ in range(2))
+            self.caches.append(sti.StiCache(k, v, *scales))
+        # pages of a sequence one after another here; any order would do, and pages may be handed out as a sequence grows
+        self.table = torch.arange(n_seqs * pages, dtype=torch.int32, device="cuda").view(n_seqs, pages)
+        self.lengths = torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
+        self.workspace = None
+
+    def stream(self, x, counts):
+        """x: float16 [sum(counts), d_model], counts[b] new tokens of sequence b -> float16 of the same shape."""
+        offsets = torch.tensor([0, *torch.tensor(counts).cumsum(0).tolist()], dtype=torch.int32, device="cuda")
+        self.lengths += torch.tensor(counts, dtype=torch.int32, device="cuda")
+        batch = sti.StiCacheBatch(self.table, self.lengths, offsets, int(x.shape[0]))
+        dh, eps = self.dims.d_head, self.dims.ln_eps
+        for (heads, qkv, bias, out, up, b1, down), p, cache in zip(self.layers, self.params, self.caches):
+            new = F.linear(x, qkv, bias).view(-1, 3, heads, dh)
+            sti.sti_cache_append(cache, batch, new[:, 1], new[:, 2])
+            context = torch.empty(x.shape[0], heads, dh, dtype=torch.float16, device="cuda")
+            need = sti.sti_cache_attention_workspace_bytes(cache, batch, heads, self.window, self.sinks)
+            if need and (self.workspace is None or self.workspace.numel() < need):
+                self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+            sti.sti_cache_attention(cache, batch, new[:, 0], context, self.workspace, window=self.window, sinks=self.sinks)
+            pre = x.float() + p.bo + F.linear(context.view(x.shape[0], -1), out).float()
+            h = F.layer_norm(pre, (x.shape[1],), p.ln1_g, p.ln1_b, eps).half()
+            pre = h.float() + p.b2 + F.linear(F.gelu(F.linear(h, up, b1)), down).float()
+            x = F.layer_norm(pre, (x.shape[1],), p.ln2_g, p.ln2_b, eps).half()
+        return x
+
+    def cached(self, layer, count):
+        """Keys and values of the first `count` positions of every sequence: float32 [n_seqs, count, heads, d_head]."""
+        cache = self.caches[layer]
+        k, v = (torch.empty(self.n_seqs, count, cache.n_kv_heads, cache.d_head, device="cuda") for _ in range(2))
+        sti.sti_cache_read(cache, sti.StiCacheBatch(self.table, self.lengths, None, 0), 0, k, v)
+        return k, v
+
+
+def main():
+    import numpy as np
+
+    import sti_synth as S
+    from paper_2207_05022_amd import device as D
+    n_seqs, tokens = 2, 90
+    wl = S.small_workload(7, S.BERT_BASE, 2, n_seqs, tokens, n_absent=3)
+    S.make_every_term_matter(wl, 7)
+    shards, params, x = D.upload_workload(wl)
+    x = x.half()
+
+    def run(chunks, **more):
+        model = StreamingSubmodel(wl.dims, shards, params, n_seqs, tokens, **more)
+        got, at = [], 0
+        for n in chunks:
+            got.append(model.stream(x[:, at:at + n].reshape(n_seqs * n, -1), [n] * n_seqs).view(n_seqs, n, -1))
+            at += n
+        return torch.cat(got, 1), model
+
+    whole, _ = run([tokens])
+    chunks = [40, 33, 1, 1, 15]
+    off = lambda a, b: float((a.float() - b.float()).norm() / b.float().norm())  # noqa: E731
+    streamed, _ = run(chunks)
+    print("chunks %s against one call, 16 bits: %.2g" % (chunks, off(streamed, whole)))
+    assert off(streamed, whole) < 2e-3      # two roundings to binary16 per layer that may fall differently
+    for bits in (8, 4):
+        other, model = run(chunks, bits=bits)
+        k, _ = model.cached(0, tokens)
+        print("%2d bits: result off by %.2g, %.0f bytes per token and head" % (bits, off(other, whole), 2 * (wl.dims.d_head * bits / 8 + 4)))
+        assert math.isfinite(float(k.sum()))
+    windowed, _ = run(chunks, window=24, sinks=4)
+    print("window of 24 and 4 first tokens: result off by %.2g" % off(windowed, whole))
+    assert np.isfinite(off(windowed, whole)) and torch.equal(windowed[:, :24], streamed[:, :24])
+
+
+if __name__ == "__main__":
+    main()

@@ -549,14 +549,15 @@ sti_status sti_cache_read(const sti_cache *cache, const sti_cache_batch *batch, 
  *     out = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale * q . k_j - max)
  * and zeros for a query that sees no key.  Keys and values that a query does not see have no part in
  * its result, whatever they hold.  Products of queries with stored values or codes and their sums are float32,
- * as are maxima, sums and the result until its one rounding; with many queries per sequence the weights w_j are
- * rounded to io_dtype (the operand type of the matrix cores) before they multiply the values, their sum is not.
+ * as are maxima, sums and the result until its one rounding; the weights w_j are rounded to the operand type of the
+ * matrix cores before they multiply the values, their sum is not: io_dtype for caches of 16 bits, binary16 for codes
+ * (beside which bfloat16 queries of 2^96 and more count as infinite).
  *
  *  n_heads      a multiple of n_kv_heads, <= 512
  *  q, out       DEVICE, rows [n_tokens] of n_heads * d_head values of io_dtype (STI_F16 or STI_BF16;
  *               that of the cache when it holds 16 bits, STI_ERR_UNSUPPORTED otherwise), strides and
  *               alignment as for sti_cache_append; not aliased.  Rows of no sequence stay as they are.
- *  scale        > 0 and finite, or 0 for 1 / sqrt(d_head) (STI_ERR_DIMS)
+ *  scale        > 0 and finite (1.44 times it, too), or 0 for 1 / sqrt(d_head) (STI_ERR_DIMS)
  *  window       >= 0, 0: all earlier tokens;  sinks >= 0, without meaning when window is 0
  *  workspace    DEVICE, >= sti_cache_attention_workspace_bytes of the same sizes, 16-byte aligned; may
  *               be NULL when that is 0.  It is that of partial results where few queries read long

@@ -652,6 +652,8 @@ def sti_cache_attention(cache: StiCache, batch: StiCacheBatch, q, out, workspace
     apart.  workspace: CUDA uint8 tensor of sti_cache_attention_workspace_bytes, or None where that is 0."""
     if q.dtype != out.dtype:
         raise ValueError("q and out must have one dtype")
+    if q.dim() != 3:
+        raise ValueError("q must be [n_tokens, n_heads, d_head]")
     heads, d = q.shape[1], cache.d_head
     st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), _row_stride(q, batch.n_tokens, heads, d, "q"),
                                  _row_stride(out, batch.n_tokens, heads, d, "out"), heads, scale, window, sinks, _ptr(workspace),

@@ -9,6 +9,7 @@ namespace {
 
 constexpr int64_t kMostPositions = (int64_t)1 << 30;   // of a sequence: sums and differences of positions and windows fit 32 bits
 constexpr int64_t kMostTokens = (int64_t)1 << 24;      // new tokens of a call
+constexpr float kLog2E = 1.44269504088896340736f;
 constexpr int64_t kMostRows = (int64_t)1 << 32;        // of a pool
 constexpr int64_t kMostBlocks = 0x7FFFFFFF;            // workgroups of a launch
 
@@ -141,7 +142,7 @@ sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *ba
     if (io_dtype != STI_F16 && io_dtype != STI_BF16) return STI_ERR_DTYPE;
     if (cache->bits == 16 && cache->dtype != io_dtype) return STI_ERR_UNSUPPORTED;
     if (!valid_heads(*cache, *batch, n_heads) || window < 0 || sinks < 0) return STI_ERR_DIMS;
-    if (!(scale >= 0.f) || !isfinite(scale)) return STI_ERR_DIMS;
+    if (!(scale >= 0.f) || !isfinite(scale * kLog2E)) return STI_ERR_DIMS;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return STI_OK;
     st = check_arrays(*cache, *batch, true);
     if (st == STI_OK) st = check_rows(q, q_stride, (int64_t)n_heads * cache->d_head, io_dtype);
@@ -161,7 +162,7 @@ sti_status sti_cache_attention(const sti_cache *cache, const sti_cache_batch *ba
     a.heads = n_heads;
     a.group = n_heads / cache->n_kv_heads;
     a.bf16 = io_dtype == STI_BF16;
-    a.scale = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->d_head)) * 1.44269504088896340736f;
+    a.scale = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->d_head)) * kLog2E;
     a.window = (int32_t)std::min<int64_t>(window, kMostPositions);
     a.sinks = (int32_t)std::min<int64_t>(sinks, kMostPositions);
     a.q = q;

@@ -18,7 +18,7 @@ __device__ inline float factor(float m, float top) { return m == top ? 1.f : __b
 // The splits' results, each shrunk to the largest maximum.  D / 4 threads of 4 features take a row's splits GROUPS at a time; the groups of a row
 // are joined through LDS.
 template <bool BF, int D, int GROUPS>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32_t heads_recip, int tile_rows, Partials partials)
+__global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, WorkCut cut, uint32_t heads_recip, Partials partials)
 {
     constexpr int WIDE = D / 4, PER_ROW = WIDE * GROUPS, ROWS = 256 / PER_ROW;
     __shared__ float4v sums[GROUPS > 1 ? GROUPS : 1][WIDE];
@@ -31,13 +31,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, uint32
     const int first = b.offsets[0], end = b.offsets[b.n_seqs];
     const RowShares shares_of = partials.rows[row];
     const int parts = shares_of.parts;
-    if (token < first || token >= end || parts == 1) return;   // (of no sequence: no tile has left anything; one share: it has left the result)
+    // rows of no sequence: no tile has left anything; one share: it has left the result; anything else that is none: offsets that are none
+    if (token < first || token >= end || parts < 2 || parts > cut.slots || shares_of.place < 0 ||
+        shares_of.place + (int64_t)(parts - 1) * a.cache.heads * cut.rows >= (int64_t)cut.slots * a.cache.heads * cut.rows)
+        return;
     const float2v *ml = (const float2v *)partials.top_weight;
     float m = -INFINITY, l = 0.f;
     float4v w = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = group; s < parts; s += GROUPS) {
-        const int64_t place = shares_of.place + (int64_t)s * a.cache.heads * tile_rows;
+        const int64_t place = shares_of.place + (int64_t)s * a.cache.heads * cut.rows;
         const float2v theirs = ml[place];
         const float4v x = *(const float4v *)(partials.sums + place * D + at * 4);
         const float t = fmaxf(m, theirs.x), f0 = factor(m, t), f1 = factor(theirs.x, t);
@@ -105,7 +108,7 @@ hipError_t launch_cache_join(const AttentionCall &a, const AttentionCut &cut, co
     const bool many = rows < 2048;
     const int64_t threads = many ? 256 : a.d / 4;
     const dim3 grid((uint32_t)((rows * threads + 255) / 256));
-    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, recip, cut.work.rows, partials); };
+    auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, cut.work, recip, partials); };
     if (a.d == 64) {
         if (a.bf16)
             many ? go(cache_join_kernel<true, 64, 16>) : go(cache_join_kernel<true, 64, 1>);

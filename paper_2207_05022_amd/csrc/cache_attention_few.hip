@@ -123,17 +123,24 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, W
         for (int i = 0; i < D / 32; ++i) qf[i] = *(const u32x4 *)(src + i * 8 / VALUES * 4 * VALUES + i * 8 % VALUES);
     }
     float4v offset = {0.f, 0.f, 0.f, 0.f};   // sums to start from: minus the queries times what the raw codes have too much
+    float back = 1.f;                        // what this lane's query's scores are multiplied by
     float key_factor = a.scale;              // what a key's sums are multiplied by, beside its scale, to be its scores
     if constexpr (BITS < 16) {
-        // the same power of two for all queries of the wave
-        float most = four_max(largest_finite<D / 32, BF>(qf));
-        most = fmaxf(most, rotated<8>(most));
-        most = fmaxf(most, rotated<4>(most));
-        most = fmaxf(most, rotated<2>(most));
-        most = fmaxf(most, rotated<1>(most));
+        // bfloat16: a power of two for each query; binary16, whose range is its own: the same for all, a part of the keys' scales
+        float most = four_max(largest_below<D / 32, BF>(qf));
+        if constexpr (!BF) {
+            most = fmaxf(most, rotated<8>(most));
+            most = fmaxf(most, rotated<4>(most));
+            most = fmaxf(most, rotated<2>(most));
+            most = fmaxf(most, rotated<1>(most));
+        }
         const int shift = query_shift<BITS == 8 ? 14 : 10>(most);
         const float into = two_to(-shift);
-        key_factor *= two_to(shift + (BITS == 8 ? 24 : 20));
+        if constexpr (BF)
+            back = two_to(shift);
+        else
+            key_factor *= two_to(shift);
+        key_factor *= BITS == 8 ? 0x1p24f : 0x1p20f;
         float total = 0.f;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
@@ -224,7 +231,7 @@ __global__ __launch_bounds__(64 * W, 2) void cache_few_kernel(AttentionCall a, W
                 const int at = g * 4 * NKB + kb * 4;
                 const float4v k4 = *(const float4v *)(sc + at), l4 = *(const float4v *)(sc + KT + at);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) s[kb][v] = fmaf(s[kb][v], k4[v], l4[v]);
+                for (int v = 0; v < 4; ++v) s[kb][v] = fmaf(BF ? s[kb][v] * back : s[kb][v], k4[v], l4[v]);
             }
         }
         if (!plain) {

@@ -67,20 +67,14 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
     const int wave_last = t.row0 + min(wr * 32 + 31, t.rows - 1);
     const int first_pos = t.base + quotient(t.row0 + min(wr * 32, t.rows - 1), a.group, cut.group_recip), last_pos = t.base + quotient(wave_last, a.group, cut.group_recip);
     u32x4 qf[D / 16];
-    float back = 1.f;   // what the scores of queries brought into binary16's range are multiplied by
+    float back = 1.f;   // what the scores of a query brought into binary16's range are multiplied by
     {
         const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + s * 16);
         if constexpr (BITS < 16 && BF) {
-            // binary16 beside codes: all queries of the wave by one power of two
-            float most = pair_max(across_32(largest_finite<D / 16, BF>(qf)));
-            most = pair_max(across_16(most));
-            most = fmaxf(most, rotated<8>(most));
-            most = fmaxf(most, rotated<4>(most));
-            most = fmaxf(most, rotated<2>(most));
-            most = fmaxf(most, rotated<1>(most));
-            const int shift = query_shift<14>(most);
+            // binary16 beside codes: a power of two for each query
+            const int shift = query_shift<14>(pair_max(across_32(largest_below<D / 16, BF>(qf))));
             const float into = two_to(-shift);
             back = two_to(shift);
 #pragma unroll

@@ -147,7 +147,7 @@ __device__ inline QueryTile find_work(const CacheView &c, const BatchView &b, co
     const int items = (int)over_all([&](const SequenceWork &q) { return (float)q.tiles * (float)shares(q.keys, per_keys); });
     int before = 0;
     const int index = items - 1 - from_last;
-    if (index < 0) return t;
+    if (index < 0 || (cut.slots > 0 && index >= cut.slots)) return t;   // (the latter: offsets that are none; there is no place for its results)
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
         if (s0 > 0) w = sequence_work(c, b, cut, s0, group, window, sinks);
         const uint32_t mine = (uint32_t)(w.tiles * shares(w.keys, per_keys)), upto = lane_scan(mine);

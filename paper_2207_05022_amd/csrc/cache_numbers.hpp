@@ -117,14 +117,15 @@ __device__ inline ValueScale value_scale(float scale)
     return {__builtin_amdgcn_logf(s), s == s ? __builtin_amdgcn_rcpf(s) : 1.f};   // (base 2; the reciprocal to one unit in the last place)
 }
 
-// Queries beside codes: values times a power of two that brings the largest finite one of a wave's queries below 2^(LOG + 1).  What is lost,
-// less than 2^-25 of a value, is 2^-(LOG + 25) of the largest.
+// Queries beside codes: values times a power of two that brings the largest below 2^(LOG + 1).  What is lost, less than 2^-25 of a value, is
+// 2^-(LOG + 25) of the largest.  Values from 2^96 on, infinities and NaN have no say in it: they become infinities or NaN, and the power of two
+// and its inverse are finite.
 __device__ inline float two_to(int e)   // -126 .. 127
 {
     return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
 }
 template <int COUNT, bool BF>
-__device__ inline float largest_finite(const cache_u32x4 (&q)[COUNT])
+__device__ inline float largest_below(const cache_u32x4 (&q)[COUNT])
 {
     float most = 0.f;
 #pragma unroll
@@ -132,7 +133,8 @@ __device__ inline float largest_finite(const cache_u32x4 (&q)[COUNT])
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t p = q[s][i] & ~odd_halves<BF>(q[s][i]);
-            most = fmaxf(most, fmaxf(fabsf(cache_number<BF>(p & 0xFFFFu)), fabsf(cache_number<BF>(p >> 16))));
+            const float x = fabsf(cache_number<BF>(p & 0xFFFFu)), y = fabsf(cache_number<BF>(p >> 16));
+            most = fmaxf(most, fmaxf(x < 0x1p96f ? x : 0.f, y < 0x1p96f ? y : 0.f));
         }
     return most;
 }

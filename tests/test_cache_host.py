@@ -48,7 +48,7 @@ BAD_CACHES = [
     (dict(bits=5), BITS), (dict(bits=0), BITS), (dict(bits=32), BITS),
     (dict(n_kv_heads=0), DIMS), (dict(n_kv_heads=65), DIMS), (dict(n_kv_heads=-1), DIMS),
     (dict(d_head=32), DIMS), (dict(d_head=96), DIMS), (dict(page_tokens=8), DIMS), (dict(page_tokens=24), DIMS),
-    (dict(page_tokens=2048), DIMS), (dict(page_tokens=0), DIMS), (dict(n_pages=-1), DIMS),
+    (dict(page_tokens=2048), DIMS), (dict(page_tokens=0), DIMS), (dict(n_pages=-1), DIMS), (dict(n_pages=1 << 26), DIMS),
     (dict(bits=16, dtype=0), DTYPE), (dict(bits=16, dtype=9), DTYPE),
     (dict(k=None), NULL), (dict(v=None), NULL), (dict(k_scale=None), NULL), (dict(bits=4, v_scale=None), NULL),
     (dict(k=FAKE + 8), ALIGN), (dict(v=FAKE + 4), ALIGN), (dict(k_scale=FAKE + 2), ALIGN), (dict(v_scale=FAKE + 1), ALIGN),
@@ -113,7 +113,7 @@ def test_attention_arguments():
     assert attend(c, b, io=0) == DTYPE and attend(c, b, io=7) == DTYPE
     assert attend(cache(bits=16, dtype=2), b, io=1) == UNSUPPORTED
     assert attend(c, b, window=-1) == DIMS and attend(c, b, sinks=-1) == DIMS
-    for scale in (-1.0, math.inf, math.nan):
+    for scale in (-1.0, math.inf, math.nan, 3.4e38):
         assert attend(c, b, scale=scale) == DIMS
 
 

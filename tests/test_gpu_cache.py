@@ -487,6 +487,48 @@ def test_a_captured_step_follows_lengths(gpu, bits):
         assert torch.isfinite(got[0][0]).all()
 
 
+@pytest.mark.parametrize("bits,new", [(8, 1), (16, 1), (4, 5), (8, 90)])
+def test_arrays_of_anything_stay_inside(gpu, bits, new):
+    """Offsets that go back or past the rows, lengths and pages of any value: nothing outside the pool and the rows is touched."""
+    torch, P = gpu
+    rng = np.random.default_rng(67)
+    s = R.make(rng, [(600, new)] * 4, 2, 64, 16, bits, "f16")
+    q, _ = queries(torch, rng, s, 4)
+    for seed in range(6):
+        g = np.random.default_rng(seed)
+        s.offsets = g.integers(-5, s.total + 9, 5).astype(np.int32)
+        s.lengths = g.choice([-2 ** 31, -1, 0, 1, 599, 10 ** 6, 2 ** 31 - 1], 4).astype(np.int32)
+        s.table = g.choice([-2 ** 31, -1, 0, 1, s.n_pages - 1, s.n_pages, 2 ** 31 - 1], s.table.shape).astype(np.int32)
+        cache, batch = R.upload(P, s)
+        need = P.sti_cache_attention_workspace_bytes(cache, batch, 4)
+        ws = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+        wide = torch.full((s.total + 64, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+        P.sti_cache_attention(cache, batch, q.cuda(), wide[32:32 + s.total], ws[:need] if need else None)
+        k = torch.randn(s.total, 2, 64, device="cuda")
+        P.sti_cache_append(cache, batch, k, k)
+        back = torch.full((6, 50, 2, 64), 7.0, device="cuda")
+        P.sti_cache_read(cache, batch, 590, back[:4], torch.empty_like(back[:4]))
+        torch.cuda.synchronize()
+        assert (wide[:32] == 7).all() and (wide[32 + s.total:] == 7).all() and (ws[need:] == 7).all() and (back[4:] == 7).all()
+
+
+@pytest.mark.parametrize("io,value", [("bf16", 1e36), ("bf16", float("inf")), ("f16", float("nan")), ("bf16", 1e25)])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new", [3, 70])
+def test_queries_of_any_size_leave_the_others_alone(gpu, io, value, bits, new):
+    """One value of one query: the other queries of its tile are within their bound."""
+    torch, P = gpu
+    rng = np.random.default_rng(71)
+    s = R.make(rng, [(50, new)], 2, 64, 16, bits, io)
+    q, exact_q = queries(torch, rng, s, 4)
+    want, bound = R.attention(s, exact_q)
+    q[1, 1, 5] = value
+    got = attend(torch, P, s, q, 4).double().numpy()
+    rest = np.ones(got.shape[:2], bool)
+    rest[1, 1] = False
+    assert (np.abs(got - want)[rest] <= bound[rest]).all()
+
+
 def test_kernels_are_timed(gpu):
     torch, P = gpu
     rng = np.random.default_rng(59)
@@ -516,3 +558,39 @@ def test_random_shapes(gpu):
         s = R.make(rng, rows, kv_heads, d, int(2 ** rng.integers(4, 8)), bits, io, fill=float("inf"))
         q, exact_q = queries(torch, rng, s, kv_heads * group, 1.5)
         check(attend(torch, P, s, q, kv_heads * group, window, sinks), *R.attention(s, exact_q, window, sinks))
+
+
+def test_the_streaming_example_runs(gpu, capsys):
+    """Chunks and single tokens through layers of shards give what one call gives; fewer bits and a window do what they say."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "streaming_submodel.py")
+    spec = importlib.util.spec_from_file_location("streaming_submodel", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    example.main()
+    assert capsys.readouterr().out.count("\n") == 4
+
+
+def test_streaming_against_the_layer_forward(gpu):
+    """A sequence of one token sees itself alone, in causal order and without: the example's layers against sti_layer_forward."""
+    import importlib.util
+    import os
+    torch, P = gpu
+    import sti_synth as S
+    from paper_2207_05022_amd import device as D
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "streaming_submodel.py")
+    spec = importlib.util.spec_from_file_location("streaming_submodel", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    wl = S.small_workload(8, S.BERT_BASE, 1, 5, 1, n_absent=4)
+    S.make_every_term_matter(wl, 8)
+    shards, params, x = D.upload_workload(wl)
+    x = x.half()
+    model = example.StreamingSubmodel(wl.dims, shards, params, 5, 16)
+    got = model.stream(x.view(5, -1), [1] * 5).float()
+    y = torch.empty_like(x)
+    ws = torch.empty(P.sti_workspace_bytes(wl.dims, 5, 1, P.STI_PREC_F16_MFMA), dtype=torch.uint8, device="cuda")
+    P.sti_layer_forward(wl.dims, shards[0], params[0], x, y, P.STI_PREC_F16_MFMA, ws)
+    off = (got - y.view(5, -1).float()).norm() / y.float().norm()
+    assert off < 3e-3      # a handful of binary16 roundings (2^-11 each) on either side
