@@ -622,9 +622,9 @@ def sti_cache_append(cache: StiCache, batch: StiCacheBatch, k, v, stream=None) -
     """k, v: CUDA tensors [n_tokens, n_kv_heads, d_head] of one dtype (float32, float16, bfloat16); rows may lie apart."""
     if k.dtype != v.dtype:
         raise ValueError("k and v must have one dtype")
-    heads, d = cache.n_kv_heads, cache.d_head
-    st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k),
-                              _row_stride(k, batch.n_tokens, heads, d, "k"), _row_stride(v, batch.n_tokens, heads, d, "v"), _stream_handle(stream))
+    rows, heads, d = batch.n_tokens, cache.n_kv_heads, cache.d_head
+    st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k), _row_stride(k, rows, heads, d, "k"),
+                              _row_stride(v, rows, heads, d, "v"), _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_cache_append")
 

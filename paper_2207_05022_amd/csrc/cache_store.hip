@@ -129,31 +129,37 @@ __device__ inline void store_row(void *pool, float *scales, int64_t row, int par
     }
 }
 
-// The sequences of up to eight rows of a wave at once: a lane per sequence, a ballot per row.
+// Position of each row's token in its sequence, for the rows of a wave (groups of LANES lanes, tokens ascending): a lane per sequence, one count of
+// the sequences that end before a token where all rows are of one, a count per row otherwise.
 template <int LANES>
 __device__ inline void find_slot(const CacheView &c, const BatchView &b, int token, int *seq, int *position)
 {
     const int lane = threadIdx.x & 63;
     *seq = -1;
     *position = -1;
+    const int first_token = __builtin_amdgcn_readlane(token, 0), last_token = __builtin_amdgcn_readlane(token, 63);
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
         const NewRows r = new_rows(b, min(s0 + lane, b.n_seqs - 1));
         const int end = s0 + lane < b.n_seqs ? r.end : 0x7FFFFFFF;
-        bool done = true;
-#pragma unroll
-        for (int g = 0; g < 64; g += LANES) {
-            const int t = __builtin_amdgcn_readlane(token, g);
-            const int n = __popcll(__ballot(end <= t));
+        // rows of `t`: those among the lanes of this test
+        auto take = [&](int t, int n, bool mine) {
             const int l = min(n, 63);
-            const int length = __builtin_amdgcn_readlane(r.length, l), last = __builtin_amdgcn_readlane(r.end, l);
-            const bool here = n < 64 && s0 + n < b.n_seqs;
-            if ((lane & ~(LANES - 1)) == g && *seq < 0 && here) {
+            if (mine && *seq < 0 && n < 64 && s0 + n < b.n_seqs) {
                 *seq = s0 + n;
-                *position = t >= __builtin_amdgcn_readlane(r.first, l) ? length - (last - t) : -1;
+                *position = t >= __builtin_amdgcn_readlane(r.first, l) ? __builtin_amdgcn_readlane(r.length, l) - (__builtin_amdgcn_readlane(r.end, l) - t) : -1;
             }
-            done &= here;
+        };
+        const int before_first = __popcll(__ballot(end <= first_token)), before_last = __popcll(__ballot(end <= last_token));
+        if (before_first == before_last) {
+            take(token, before_first, true);
+        } else {
+#pragma unroll
+            for (int g = 0; g < 64; g += LANES) {
+                const int t = __builtin_amdgcn_readlane(token, g);
+                take(t, __popcll(__ballot(end <= t)), (lane & ~(LANES - 1)) == g);
+            }
         }
-        if (done) break;
+        if (before_last < 64) break;
     }
     if (*position >= cache_capacity(c, b)) *position = -1;
     if (*position < 0) *seq = -1;
