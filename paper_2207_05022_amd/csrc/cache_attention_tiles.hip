@@ -39,6 +39,9 @@ struct TileShape {
     static constexpr int STAGE_BYTES = STEP_BYTES * BUFFERS * WK;
     static constexpr int LDS_BYTES = STAGE_BYTES > JOIN_FLOATS * 4 ? STAGE_BYTES : JOIN_FLOATS * 4;
     static_assert(KT * ROW_CHUNKS % THREADS == 0, "");
+    // Feature at place p of a row in LDS.  Codes: the first halves of all requests, then the second ones, so that lanes behind each other write bytes
+    // behind each other (in the order of the features each write took its LDS banks twice).
+    __device__ static constexpr int feature(int p) { return BITS == 16 ? p : p % (D / 2) / 8 * 16 + p / (D / 2) * 8 + p % 8; }
 };
 
 template <int BITS, bool BF, int D, int WR, int WK>
@@ -69,9 +72,9 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
     u32x4 qf[D / 16];
     float back = 1.f;   // what the scores of a query brought into binary16's range are multiplied by
     {
-        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + g * 8;
+        const uint16_t *src = (const uint16_t *)a.q + (t.first + token) * a.q_stride + q_head * D + T::feature(g * 8);
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + s * 16);
+        for (int s = 0; s < D / 16; ++s) qf[s] = *(const u32x4 *)(src + T::feature(s * 16));
         if constexpr (BITS < 16 && BF) {
             // binary16 beside codes: a power of two for each query
             const int shift = query_shift<14>(pair_max(across_32(largest_below<D / 16, BF>(qf))));
@@ -155,21 +158,22 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
         uint16_t *ks = (uint16_t *)step_lds(buffer), *vs = ks + KT * KS;
 #pragma unroll
         for (int i = 0; i < T::ITEMS; ++i) {
-            const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, at = item % T::ROW_CHUNKS * T::CHUNK;
+            const int item = i * T::THREADS + tid, r = item / T::ROW_CHUNKS, at = item % T::ROW_CHUNKS * 8;
             u32x4 *kd = (u32x4 *)(ks + r * KS + at), *vd = (u32x4 *)(vs + r * VS + at);
+            constexpr int SECOND = D / 2 / 8;
             if constexpr (BITS == 16) {
                 kd[0] = rows.k[i];
                 vd[0] = rows.v[i];
             } else if constexpr (BITS == 8) {
                 kd[0] = numbers_of_bytes(rows.k[i][0], rows.k[i][1]);
-                kd[1] = numbers_of_bytes(rows.k[i][2], rows.k[i][3]);
+                kd[SECOND] = numbers_of_bytes(rows.k[i][2], rows.k[i][3]);
                 vd[0] = numbers_of_bytes(rows.v[i][0], rows.v[i][1]);
-                vd[1] = numbers_of_bytes(rows.v[i][2], rows.v[i][3]);
+                vd[SECOND] = numbers_of_bytes(rows.v[i][2], rows.v[i][3]);
             } else {
                 kd[0] = numbers_of_nibbles(rows.k[i][0]);
-                kd[1] = numbers_of_nibbles(rows.k[i][1]);
+                kd[SECOND] = numbers_of_nibbles(rows.k[i][1]);
                 vd[0] = numbers_of_nibbles(rows.v[i][0]);
-                vd[1] = numbers_of_nibbles(rows.v[i][1]);
+                vd[SECOND] = numbers_of_nibbles(rows.v[i][1]);
             }
         }
         if constexpr (BITS < 16) {
@@ -354,14 +358,14 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
 #pragma unroll
                 for (int v4 = 0; v4 < 4; ++v4) {
                     const u32x2 w = {cache_pair<BF>(o[e][v4 * 4] * inv, o[e][v4 * 4 + 1] * inv), cache_pair<BF>(o[e][v4 * 4 + 2] * inv, o[e][v4 * 4 + 3] * inv)};
-                    *(u32x2 *)(out + e * 32 + v4 * 8) = w;
+                    *(u32x2 *)(out + T::feature(e * 32 + v4 * 8)) = w;
                 }
         } else {
             float *out = partials.sums + place * D + g * 4;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-                for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(out + e * 32 + v4 * 8) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
+                for (int v4 = 0; v4 < 4; ++v4) *(float4v *)(out + T::feature(e * 32 + v4 * 8)) = float4v{o[e][v4 * 4], o[e][v4 * 4 + 1], o[e][v4 * 4 + 2], o[e][v4 * 4 + 3]};
         }
         if (cut.slots > 0 && g == 0) {
             partials.top_weight[place * 2] = top;
@@ -402,9 +406,9 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void cache_tiles_kernel(AttentionC
             if (t.parts == 1) {
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
                 const u32x2 w = {cache_pair<BF>(v[0] * inv, v[1] * inv), cache_pair<BF>(v[2] * inv, v[3] * inv)};
-                *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + at) = w;
+                *(u32x2 *)((uint16_t *)a.out + (t.first + tok) * a.out_stride + qh * D + T::feature(at)) = w;
             } else {
-                *(float4v *)(partials.sums + place * D + at) = v;
+                *(float4v *)(partials.sums + place * D + T::feature(at)) = v;
             }
             if (cut.slots > 0 && at == 0) {
                 partials.top_weight[place * 2] = m;
