@@ -85,12 +85,12 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     w.token_rows = (w.rows + group - 2) / group + 1;   // (a tile may begin and end inside a token's heads)
     w.group_recip = reciprocal((uint32_t)group);
     w.heads_recip = reciprocal((uint32_t)kv_heads);
-    w.least_keys = 256;
+    w.least_keys = w.rows == 16 && d == 64 ? 256 : 128;
     int64_t keys = capacity;   // the most that a tile's queries see
     if (window > 0) keys = std::min(keys, (int64_t)window + sinks + w.token_rows);
     // Tiles for fewer than two workgroups per compute unit: shares for one round of as many as are resident
     const int64_t tiles = tile_bound(n_tokens, n_seqs, group, w.rows), slots = (w.rows == 16 && d == 64 ? 1024 : 512) / kv_heads;
-    w.slots = tiles * kv_heads < 512 && keys >= 2 * w.least_keys ? (int32_t)slots : 0;
+    w.slots = tiles * kv_heads < 512 && keys >= 512 ? (int32_t)slots : 0;
     cut.blocks = (w.slots > 0 ? slots : tiles) * kv_heads;
     return cut;
 }

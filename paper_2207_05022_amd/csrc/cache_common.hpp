@@ -122,7 +122,9 @@ __device__ inline QueryTile find_work(const CacheView &c, const BatchView &b, co
     };
     float per_keys = 0.f;   // 1 / the keys of a share
     if (cut.slots > 0) {
-        float low = fmaxf(over_all([](const SequenceWork &q) { return (float)q.tiles * (float)q.keys; }) / (float)cut.slots, (float)cut.least_keys);
+        const float all_keys = over_all([](const SequenceWork &q) { return (float)q.tiles * (float)q.keys; });
+        const float one_round = all_keys * (1.f / 256.f) * (float)c.heads;   // keys of a share with one workgroup on each of the 256 compute units
+        float low = fmaxf(all_keys / (float)cut.slots, fminf(fmaxf(one_round, (float)cut.least_keys), 256.f));
         float high = 0x1p31f;   // one share each
         auto fits = [&](float keys) {
             const float per = 1.f / keys;
