@@ -16,7 +16,8 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 __device__ inline float factor(float m, float top) { return m == top ? 1.f : __builtin_amdgcn_exp2f(m - top); }   // (both -inf: 1)
 
 // The splits' results, each shrunk to the largest maximum.  D / 4 threads of 4 features take a row's splits GROUPS at a time; the groups of a row
-// are joined through LDS.
+// are joined through LDS.  4.6 to 5.8 us: start-up, the chain row -> its shares -> their results, and for many rows what the shares have left (1135 tokens
+// of 16 heads of 64 in two to four shares: 14 MB).
 template <bool BF, int D, int GROUPS>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttentionCall a, WorkCut cut, uint32_t heads_recip, Partials partials)
 {
@@ -81,14 +82,21 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     const int64_t rows = (n_tokens + n_seqs - 1) / n_seqs * group;
     AttentionCut cut;
     WorkCut &w = cut.work;
+    // 16: no barrier, all requests for whole rows (2 sequences of 230,634 keys, 4 heads on one: 64 us, in a tile of 32 of the other kernel 131).  64:
+    // two groups of waves on a tile (40 rows of five tokens: 31.5 us against 36 in tiles of 128).  128: each key's row from LDS for twice the
+    // queries (5612 tokens behind up to 16384: 1122 us against 1389 in tiles of 64, a window of 512 over 7919 tokens 40 against 50).
     w.rows = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
     w.token_rows = (w.rows + group - 2) / group + 1;   // (a tile may begin and end inside a token's heads)
     w.group_recip = reciprocal((uint32_t)group);
     w.heads_recip = reciprocal((uint32_t)kv_heads);
+    // Shares of at least so many keys while compute units are idle, of 256 otherwise (find_work).  128 in place of 256: two drafts of five behind 2000
+    // keys 15.4 -> 13.7 us; 16 rows of 64: 4000 keys of 12 heads 10.4 -> 11.0, the four waves' start costs more than what it hides.  64: 13.7 -> 15.0.
     w.least_keys = w.rows == 16 && d == 64 ? 256 : 128;
     int64_t keys = capacity;   // the most that a tile's queries see
     if (window > 0) keys = std::min(keys, (int64_t)window + sinks + w.token_rows);
-    // Tiles for fewer than two workgroups per compute unit: shares for one round of as many as are resident
+    // Tiles for fewer than two workgroups per compute unit: shares for one round of as many as are resident (128 queries: 512 shares 75 us, 768 104, 1024
+    // 79; 16 of 64: 1024 34.1 against 38.6 for 512; 16 of 128: 512 55.7 against 64 for 1024).  No shares of more tiles (576 of a window of 1028 keys:
+    // 29.6 us, in shares 33), nor of fewer than 512 keys, for which joining costs more than waiting (273 keys of two heads: 8.9 us, in shares 10.7).
     const int64_t tiles = tile_bound(n_tokens, n_seqs, group, w.rows), slots = (w.rows == 16 && d == 64 ? 1024 : 512) / kv_heads;
     w.slots = tiles * kv_heads < 512 && keys >= 512 ? (int32_t)slots : 0;
     cut.blocks = (w.slots > 0 ? slots : tiles) * kv_heads;
@@ -105,20 +113,20 @@ hipError_t launch_cache_join(const AttentionCall &a, const AttentionCut &cut, co
     const int64_t rows = (int64_t)a.batch.n_tokens * a.heads;
     const uint32_t recip = reciprocal((uint32_t)a.heads);
     // many rows: each to D / 4 threads; few (many shares, then): each to a workgroup
-    const bool many = rows < 2048;
-    const int64_t threads = many ? 256 : a.d / 4;
+    const bool few = rows < 2048;
+    const int64_t threads = few ? 256 : a.d / 4;
     const dim3 grid((uint32_t)((rows * threads + 255) / 256));
     auto go = [&](auto kernel) { launch(kernel, grid, dim3(256), 0, stream, a, cut.work, recip, partials); };
     if (a.d == 64) {
         if (a.bf16)
-            many ? go(cache_join_kernel<true, 64, 16>) : go(cache_join_kernel<true, 64, 1>);
+            few ? go(cache_join_kernel<true, 64, 16>) : go(cache_join_kernel<true, 64, 1>);
         else
-            many ? go(cache_join_kernel<false, 64, 16>) : go(cache_join_kernel<false, 64, 1>);
+            few ? go(cache_join_kernel<false, 64, 16>) : go(cache_join_kernel<false, 64, 1>);
     } else {
         if (a.bf16)
-            many ? go(cache_join_kernel<true, 128, 8>) : go(cache_join_kernel<true, 128, 1>);
+            few ? go(cache_join_kernel<true, 128, 8>) : go(cache_join_kernel<true, 128, 1>);
         else
-            many ? go(cache_join_kernel<false, 128, 8>) : go(cache_join_kernel<false, 128, 1>);
+            few ? go(cache_join_kernel<false, 128, 8>) : go(cache_join_kernel<false, 128, 1>);
     }
     return hipGetLastError();
 }

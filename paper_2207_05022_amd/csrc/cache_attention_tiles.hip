@@ -5,6 +5,15 @@
 // the registers where they are, and the maximum of a query crosses only lanes l and l ^ 32.  The formula with scales is that of
 // cache_attention_few.hip.  Keys and values of a step go through registers to LDS (codes become binary16 on the way), one step ahead of the
 // products; V^T is read from its rows by the transposing LDS read.
+//
+// Bound by the vector units and the matrix cores together: a step of 64 keys of 128 values in 8 bits is about 320 vector instructions and 32 products
+// of a wave, and the two pipes of a unit overlap by about a quarter (measured alone, with one kind of wave or two).  Of the vector instructions
+// 87 make binary16 numbers of codes, which a tile's four waves share, and 160 are the softmax, 5 to a score.  128 queries to a tile (64 where there are
+// no more: then two groups of waves take every other step, so that all four have work), two workgroups to a compute unit or three at 64 values.
+// Measured (kernel alone): 5612 tokens of 2 sequences behind up to 16384, 16 heads on 4 of 128 in 8 bits, 728 GFLOP, 935 us, 0.78 PFLOP/s (vector
+// units busy for 52 % of it, matrix cores 37 %, LDS 43 %); 1135 tokens of 4 sequences behind up to 8192, 16 heads of 64 in bfloat16, 29 GFLOP, 66 us, 0.45 PFLOP/s;
+// a window of 512 over 7919 tokens, 12 heads of 64, 12 GFLOP, 37.6 us, 0.33 PFLOP/s (a tile of 128 queries walks 640 keys for the 512 that each sees); 33
+// tokens of 8 sequences with 8 heads on one, 42,870 keys of 4 heads of 128 in 16 bits, 88 MB, 21 us, 4.1 TB/s.
 #include "cache_numbers.hpp"
 
 namespace sti {
@@ -26,9 +35,9 @@ __device__ inline float16v product(u32x4 a, u32x4 b, float16v c)
 }
 template <int BITS, int D, int WR, int WK>
 struct TileShape {
-    static constexpr int KT = WR >= 4 ? 64 : 32;         // keys of a step
+    static constexpr int KT = WR >= 4 ? 64 : 32;         // keys of a step (32 for 128 queries: a barrier for half of the work; slower)
     static constexpr int BUFFERS = 2;
-    static constexpr int AHEAD = BITS == 16 && D == 128 ? 1 : 2;   // steps whose rows are in registers (16-bit rows of 128 values: no room for two)
+    static constexpr int AHEAD = BITS == 16 && D == 128 ? 1 : 2;   // steps whose rows are in registers (16-bit rows of 128 values: no room for two; 960 -> 952 us)
     static constexpr int THREADS = 64 * WR;              // of a group
     static constexpr int KS = D + 8, VS = D + 32;        // halves per row in LDS: no two lanes of a read share a bank
     static constexpr int CHUNK = BITS == 16 ? 8 : 16;    // values of a request: 16 bytes, 8 of codes of 4 bits

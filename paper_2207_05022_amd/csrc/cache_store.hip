@@ -5,6 +5,10 @@
 // One scale per token and key/value head: the attention multiplies a score and a weight by it, never a single value.  A row is
 // d / 8 lanes of 8 values: one or two 16-byte requests per lane and matrix, the maximum over the lanes by DPP.  Both kernels are bound by
 // memory and, for few rows, by the chain offsets -> page -> row.
+//
+// Measured (kernel alone): one token of 12 heads of 64 in 4 bits 3.7 us to write and 3.0 to read its 38 positions back, start-up and that chain;
+// 3953 tokens of 12 heads of 64 in 8 bits, 18 MB, 8.0 us to write; 24 sequences of up to 2001 positions, 16 heads of 64 in 16 bits, 334 MB, 45 us to
+// read back, and 4 of up to 16896, 8 heads of 128 in 4 bits, 330 MB, 45 us: 7.4 TB/s (part of the pools comes from the cache in front of memory).
 #include "cache_common.hpp"
 
 namespace sti {
@@ -165,13 +169,15 @@ __device__ inline void find_slot(const CacheView &c, const BatchView &b, int tok
     if (*position < 0) *seq = -1;
 }
 
+// A row to a group of lanes, keys and values together, so that what a token's slot is found from is read once; the rows are asked for in front of it.
 template <int BITS, sti_dtype STORED, sti_dtype IO, int D>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchView b, const void *k, const void *v, int64_t k_stride,
                                                            int64_t v_stride, uint32_t heads_recip)
 {
     constexpr int LANES = D / 8, ROWS = 256 / LANES;
     const int part = threadIdx.x % LANES;
-    // rows in the order (8 tokens, head, token): the slots of 8 tokens of a sequence lie behind each other in a page
+    // rows in the order (8 tokens, head, token): the slots of 8 tokens of a sequence lie behind each other in a page (by token and head, whose slots lie
+    // a page's row apart: 9.1 us in place of 8.9 for the 3953 tokens above)
     const int row = (int)(blockIdx.x * ROWS + threadIdx.x / LANES);
     const int eight = quotient(row >> 3, c.heads, heads_recip), head = (row >> 3) - eight * c.heads;
     const int token_in = eight * 8 + (row & 7), token = min(token_in, b.n_tokens - 1);
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
             load_row<BITS, STORED, D>(c.v, c.v_scale, at, part, xv);
         }
         const int64_t to = (((int64_t)seq * count + j) * c.heads + head) * D + part * 8;
-        store8<OUT, true>(k_out, to, xk);   // (past the caches: what is read back of long sequences is more than they hold; 84 -> 51 us for 335 MB)
+        store8<OUT, true>(k_out, to, xk);   // (past the caches: what is read back of long sequences is more than they hold; append and read 84 -> 51 us for 335 MB)
         store8<OUT, true>(v_out, to, xv);
     }
 }
