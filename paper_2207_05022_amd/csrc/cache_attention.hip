@@ -94,8 +94,8 @@ AttentionCut attention_cut(int64_t n_tokens, int n_seqs, int heads, int kv_heads
     w.least_keys = w.rows == 16 && d == 64 ? 256 : 128;
     int64_t keys = capacity;   // the most that a tile's queries see
     if (window > 0) keys = std::min(keys, (int64_t)window + sinks + w.token_rows);
-    // Tiles for fewer than two workgroups per compute unit: shares for one round of as many as are resident (128 queries: 512 shares 75 us, 768 104, 1024
-    // 79; 16 of 64: 1024 34.1 against 38.6 for 512; 16 of 128: 512 55.7 against 64 for 1024).  No shares of more tiles (576 of a window of 1028 keys:
+    // Tiles for fewer than two workgroups per compute unit: shares for one round of as many as are resident (128 queries: 512 shares 66 us,
+    // 1024 71; 16 of 64: 1024 35.4, 512 38.6, 1536 36.9; 16 of 128: 512 56.3, 768 69, 1024 62).  No shares of more tiles (576 of a window of 1028 keys:
     // 29.6 us, in shares 33), nor of fewer than 512 keys, for which joining costs more than waiting (273 keys of two heads: 8.9 us, in shares 10.7).
     const int64_t tiles = tile_bound(n_tokens, n_seqs, group, w.rows), slots = (w.rows == 16 && d == 64 ? 1024 : 512) / kv_heads;
     w.slots = tiles * kv_heads < 512 && keys >= 512 ? (int32_t)slots : 0;

@@ -12,7 +12,8 @@
 // S^T; only the values go through LDS, as stored, to be read transposed by the LDS reads for 16, 8 and 4 bits.  The maximum and the sum of a query
 // are per lane, over its 4 lanes at the end of a step.  What is asked for in a step is used in the next; waves hide what is left of the way.
 //
-// Bound by memory: a key's row is read once and used for all queries of its head, and 16 columns cost the matrix cores what one would.  Four waves
+// Bound by memory, in 8 and 4 bits with the vector units busy for 60 % (making numbers of codes, scales, the softmax): a key's row is read once and
+// used for all queries of its head, and 16 columns cost the matrix cores what one would.  Four waves
 // with steps of their own and no barrier before the end, so that a step's wait holds up nobody else; 32 keys to a step, or 64 of 4 bits, for 8 to 16
 // requests of a lane on their way (eight waves to a workgroup: 10 % slower).  Measured (kernel alone): a token each of 32 sequences of 84,574 keys,
 // 12 heads of 64 in 8 bits, 138 MB, 29 us, 4.7 TB/s; of 2 sequences of 230,634 keys, 32 heads on 8 of 128 in 4 bits, 251 MB, 44.7 us, 5.6 TB/s;

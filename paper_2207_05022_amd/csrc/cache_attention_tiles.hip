@@ -11,7 +11,7 @@
 // 87 make binary16 numbers of codes, which a tile's four waves share, and 160 are the softmax, 5 to a score.  128 queries to a tile (64 where there are
 // no more: then two groups of waves take every other step, so that all four have work), two workgroups to a compute unit or three at 64 values.
 // Measured (kernel alone): 5612 tokens of 2 sequences behind up to 16384, 16 heads on 4 of 128 in 8 bits, 728 GFLOP, 935 us, 0.78 PFLOP/s (vector
-// units busy for 52 % of it, matrix cores 37 %, LDS 43 %); 1135 tokens of 4 sequences behind up to 8192, 16 heads of 64 in bfloat16, 29 GFLOP, 66 us, 0.45 PFLOP/s;
+// units busy for 53 % of it, matrix cores 38 %, LDS 44 %); 1135 tokens of 4 sequences behind up to 8192, 16 heads of 64 in bfloat16, 29 GFLOP, 66 us, 0.45 PFLOP/s;
 // a window of 512 over 7919 tokens, 12 heads of 64, 12 GFLOP, 37.6 us, 0.33 PFLOP/s (a tile of 128 queries walks 640 keys for the 512 that each sees); 33
 // tokens of 8 sequences with 8 heads on one, 42,870 keys of 4 heads of 128 in 16 bits, 88 MB, 21 us, 4.1 TB/s.
 #include "cache_numbers.hpp"
