@@ -580,6 +580,7 @@ class StiCache:
         else:
             k_scale = v_scale = None
         self.k, self.v, self.k_scale, self.v_scale, self.bits = k, v, k_scale, v_scale, bits
+        self.on_gpu = all(t is None or t.is_cuda for t in (k, v, k_scale, v_scale))
         self.n_pages, self.n_kv_heads, self.page_tokens = (int(n) for n in k.shape[:3])
         self.d_head = int(k.shape[3]) * (2 if bits == 4 else 1)
         self.struct = StiCacheStruct(self.n_kv_heads, self.d_head, bits, self.page_tokens, self.n_pages,
@@ -601,6 +602,7 @@ class StiCacheBatch:
         if page_table.shape[0] != n_seqs or (offsets is not None and offsets.shape[0] != n_seqs + 1):
             raise ValueError("page_table has a row, and offsets an entry and one more, for each of lengths")
         self.page_table, self.lengths, self.offsets = page_table, lengths, offsets
+        self.on_gpu = all(t.is_cuda for t, _ in shapes)
         self.n_seqs, self.n_tokens, self.max_pages = n_seqs, int(n_tokens), int(page_table.shape[1])
         self.struct = StiCacheBatchStruct(n_seqs, self.n_tokens, self.max_pages, _ptr(page_table), _ptr(lengths), _ptr(offsets))
         self.ref = C.byref(self.struct)
@@ -618,13 +620,18 @@ def _row_stride(t, n_tokens: int, heads: int, d_head: int, name: str) -> int:
     return strides[0] if n_tokens > 1 else heads * d_head
 
 
+_ON_GPU = "the tensors of a cache, a batch and a call must be CUDA tensors"
+
+
 def sti_cache_append(cache: StiCache, batch: StiCacheBatch, k, v, stream=None) -> None:
     """k, v: CUDA tensors [n_tokens, n_kv_heads, d_head] of one dtype (float32, float16, bfloat16); rows may lie apart."""
     if k.dtype != v.dtype:
         raise ValueError("k and v must have one dtype")
     rows, heads, d = batch.n_tokens, cache.n_kv_heads, cache.d_head
-    st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k), _row_stride(k, rows, heads, d, "k"),
-                              _row_stride(v, rows, heads, d, "v"), _stream_handle(stream))
+    k_stride, v_stride = _row_stride(k, rows, heads, d, "k"), _row_stride(v, rows, heads, d, "v")
+    if not (k.is_cuda and v.is_cuda and cache.on_gpu and batch.on_gpu):
+        raise ValueError(_ON_GPU)
+    st = lib.sti_cache_append(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _dtype_code(k), k_stride, v_stride, _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_cache_append")
 
@@ -636,6 +643,8 @@ def sti_cache_read(cache: StiCache, batch: StiCacheBatch, first: int, k_out, v_o
         raise ValueError("k_out and v_out must be [n_seqs, count, n_kv_heads, d_head]")
     if k_out.dtype != v_out.dtype or not k_out.is_contiguous() or not v_out.is_contiguous():
         raise ValueError("k_out and v_out must be contiguous and of one dtype")
+    if not (k_out.is_cuda and v_out.is_cuda and cache.on_gpu and batch.on_gpu):
+        raise ValueError(_ON_GPU)
     st = lib.sti_cache_read(cache.ref, batch.ref, int(first), shape[1], k_out.data_ptr(), v_out.data_ptr(), _dtype_code(k_out),
                             _stream_handle(stream))
     if st != 0:
@@ -655,8 +664,10 @@ def sti_cache_attention(cache: StiCache, batch: StiCacheBatch, q, out, workspace
     if q.dim() != 3:
         raise ValueError("q must be [n_tokens, n_heads, d_head]")
     heads, d = q.shape[1], cache.d_head
-    st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), _row_stride(q, batch.n_tokens, heads, d, "q"),
-                                 _row_stride(out, batch.n_tokens, heads, d, "out"), heads, scale, window, sinks, _ptr(workspace),
-                                 _nbytes(workspace), _stream_handle(stream))
+    q_stride, out_stride = _row_stride(q, batch.n_tokens, heads, d, "q"), _row_stride(out, batch.n_tokens, heads, d, "out")
+    if not (q.is_cuda and out.is_cuda and cache.on_gpu and batch.on_gpu and (workspace is None or workspace.is_cuda)):
+        raise ValueError(_ON_GPU)
+    st = lib.sti_cache_attention(cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _dtype_code(q), q_stride, out_stride, heads, scale, window,
+                                 sinks, _ptr(workspace), _nbytes(workspace), _stream_handle(stream))
     if st != 0:
         raise StiError(st, "sti_cache_attention")

@@ -169,3 +169,15 @@ def test_python_checks():
         P.sti_cache_attention(c, b, half(1, 64, 2).transpose(1, 2), half(1, 2, 64))
     with pytest.raises(ValueError):
         P.sti_cache_read(c, b, 0, half(1, 4, 1, 128), half(1, 4, 1, 128))
+
+
+def test_tensors_of_the_host_are_refused():
+    import torch
+    half = lambda *s: torch.zeros(*s, dtype=torch.float16)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)
+    c, b = P.StiCache(half(2, 1, 16, 64), half(2, 1, 16, 64)), P.StiCacheBatch(ints(0, 1).view(1, 2), ints(3), ints(0, 1), 1)
+    row, back = half(1, 1, 64), half(1, 4, 1, 64)
+    for call in (lambda: P.sti_cache_append(c, b, row, row), lambda: P.sti_cache_read(c, b, 0, back, back),
+                 lambda: P.sti_cache_attention(c, b, row, row)):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
